@@ -82,7 +82,8 @@ enum rrq_status {
     RRQ_ERR_STAGES = 5, /* n_stages not in 1..RRQ_MAX_STAGES, or k_stages not in 1..n_stages */
     RRQ_ERR_DTYPE = 6,  /* out_dtype not one of enum rrq_dtype */
     RRQ_ERR_HIP = 7,    /* the HIP runtime reported an error while launching */
-    RRQ_ERR_FORMAT = 8  /* zero_point or scale_type not one of the enums below */
+    RRQ_ERR_FORMAT = 8, /* zero_point or scale_type not one of the enums below */
+    RRQ_ERR_WORKSPACE = 9 /* rrq_serve.h: workspace_bytes smaller than the call needs */
 };
 
 /* Output element type of rrq_reconstruct. */

@@ -8,7 +8,9 @@ C ABI (``rrq_construct``, ``rrq_construct_many``, ``rrq_construct_from_base``, `
 arguments: tensors become device pointers,
 the stream defaults to torch's current stream, and a nonzero status raises
 ``RRQError``. ``construct``, ``construct_from_base``, ``reconstruct`` and
-``linear`` additionally allocate the output tensors with torch. Every computation runs in the HIP kernels; there is
+``linear`` additionally allocate the output tensors with torch. ``serving`` binds
+include/rrq_serve.h (the 8-bit cache, attention over it, token scoring); its names
+are available here too. Every computation runs in the HIP kernels; there is
 no fallback, and a missing library raises.
 """
 
@@ -31,6 +33,7 @@ RRQ_ERR_STAGES = 5
 RRQ_ERR_DTYPE = 6
 RRQ_ERR_HIP = 7
 RRQ_ERR_FORMAT = 8
+RRQ_ERR_WORKSPACE = 9
 
 RRQ_ZP_INTEGER = 0
 RRQ_ZP_REAL = 1
@@ -399,3 +402,10 @@ def group_pmr(W, group_size: int = 128, stream=None):
     out = torch.empty(rows * cols // group_size, dtype=torch.float32, device=W.device)
     rrq_group_pmr(W, rows, cols, group_size, out, stream)
     return out
+
+
+from .serving import (  # noqa: E402,F401  (uses the names above)
+    CODE_TYPES, RRQ_CODE_FP8, RRQ_CODE_INT8, RRQ_MAX_TOP, CacheBatch, KVCache, RrqBatch, RrqCache,
+    attention_workspace, cache_attention, cache_read, cache_write, logprobs_workspace,
+    rrq_cache_attention, rrq_cache_attention_workspace, rrq_cache_read, rrq_cache_write,
+    rrq_token_logprobs, rrq_token_logprobs_workspace, token_logprobs)

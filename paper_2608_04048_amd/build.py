@@ -43,7 +43,8 @@ SOURCE_FLAGS = {"rrq_linear": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
                 "rrq_decode": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
                 "rrq_batch": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
                 "rrq_prefill": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
-                "rrq_split": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+                "rrq_split": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"],
+                "rrq_attention": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
 
 
 def hipcc() -> str:
@@ -71,7 +72,7 @@ def build(keep_asm: bool = False) -> str:
     os.makedirs(BUILD_DIR, exist_ok=True)
     kern_objs, cmds = [], []
     for name in ("rrq_kernels", "rrq_linear", "rrq_decode", "rrq_batch", "rrq_prefill",
-                 "rrq_split"):
+                 "rrq_split", "rrq_cache", "rrq_attention", "rrq_logprobs"):
         obj = os.path.join(BUILD_DIR, name + ".o")
         cmd = [cc, *DEVICE_FLAGS, *SOURCE_FLAGS.get(name, []), f"-I{INCLUDE}", f"-I{CSRC}", "-c",
                os.path.join(CSRC, name + ".hip"), "-o", obj]
@@ -81,12 +82,15 @@ def build(keep_asm: bool = False) -> str:
         kern_objs.append(obj)
     with ThreadPoolExecutor(max_workers=len(cmds)) as pool:
         list(pool.map(_run, cmds))
-    api_obj = os.path.join(BUILD_DIR, "rrq_api.o")
-    _run([cc, "-x", "c++", *HOST_FLAGS, "-D__HIP_PLATFORM_AMD__", f"-I{INCLUDE}", f"-I{CSRC}",
-          f"-I{ROCM}/include",
-          "-c", os.path.join(CSRC, "rrq_api.cpp"), "-o", api_obj])
+    api_objs = []
+    for name in ("rrq_api", "rrq_serve_api"):
+        obj = os.path.join(BUILD_DIR, name + ".o")
+        _run([cc, "-x", "c++", *HOST_FLAGS, "-D__HIP_PLATFORM_AMD__", f"-I{INCLUDE}", f"-I{CSRC}",
+              f"-I{ROCM}/include",
+              "-c", os.path.join(CSRC, name + ".cpp"), "-o", obj])
+        api_objs.append(obj)
     tmp = LIB + ".tmp"
-    _run([cc, f"--offload-arch={ARCH}", "-shared", "-fPIC", *kern_objs, api_obj, "-o", tmp])
+    _run([cc, f"--offload-arch={ARCH}", "-shared", "-fPIC", *kern_objs, *api_objs, "-o", tmp])
     os.replace(tmp, LIB)
     build_probe()
     return LIB

@@ -346,6 +346,7 @@ extern "C" const char *rrq_status_string(int status)
     case RRQ_ERR_DTYPE: return "out_dtype must be RRQ_F32 or RRQ_BF16";
     case RRQ_ERR_HIP: return "the HIP runtime reported an error";
     case RRQ_ERR_FORMAT: return "zero_point must be an enum rrq_zero_point value and scale_type an enum rrq_scale_type value";
+    case RRQ_ERR_WORKSPACE: return "the workspace is smaller than the call needs";
     default: return "unknown status";
     }
 }
