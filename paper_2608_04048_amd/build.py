@@ -72,7 +72,8 @@ def build(keep_asm: bool = False) -> str:
     os.makedirs(BUILD_DIR, exist_ok=True)
     kern_objs, cmds = [], []
     for name in ("rrq_kernels", "rrq_linear", "rrq_decode", "rrq_batch", "rrq_prefill",
-                 "rrq_split", "rrq_cache", "rrq_attention", "rrq_logprobs"):
+                 "rrq_split", "rrq_cache", "rrq_attention",
+                 "rrq_attention_rows", "rrq_logprobs"):
         obj = os.path.join(BUILD_DIR, name + ".o")
         cmd = [cc, *DEVICE_FLAGS, *SOURCE_FLAGS.get(name, []), f"-I{INCLUDE}", f"-I{CSRC}", "-c",
                os.path.join(CSRC, name + ".hip"), "-o", obj]

@@ -15,6 +15,13 @@ namespace {
 struct PageSlot {
     int64_t page, row0;
     int lo, hi;
+
+    // The row of a slot, from row0; of the nearest new slot for the others, so
+    // that loads need no branch (such a row changes no maximum).
+    __device__ __forceinline__ int near(int slot) const
+    {
+        return (slot < lo ? lo : (slot >= hi ? hi - 1 : slot)) - lo;
+    }
 };
 
 __device__ __forceinline__ bool find_page(const rrq_cache &c, const rrq_batch &b, int64_t u,
@@ -114,10 +121,7 @@ __global__ __launch_bounds__(1024) void cache_write_kernel(CacheWrite a)
 #pragma unroll
         for (int i = 0; i < kTok; ++i) {
             const int slot = slot0 + i * tokens;
-            x[i] = f32x4{0, 0, 0, 0};
-            if (slot >= p.lo && slot < p.hi)
-                x[i] = load4<BF16>(a.K, (p.row0 + slot - p.lo) * a.k_token + head * a.k_head +
-                                            4 * c);
+            x[i] = load4<BF16>(a.K, (p.row0 + p.near(slot)) * a.k_token + head * a.k_head + 4 * c);
         }
         const float stored = p.lo > 0 ? *scale : 0.0f;
 #pragma unroll
@@ -148,10 +152,7 @@ __global__ __launch_bounds__(1024) void cache_write_kernel(CacheWrite a)
 #pragma unroll
         for (int i = 0; i < kRun; ++i) {
             const int slot = slot0 + i;
-            x[i] = f32x2{0, 0};
-            if (active && slot >= p.lo && slot < p.hi)
-                x[i] = load2<BF16>(a.V, (p.row0 + slot - p.lo) * a.v_token + head * a.v_head +
-                                            2 * c);
+            x[i] = load2<BF16>(a.V, (p.row0 + p.near(slot)) * a.v_token + head * a.v_head + 2 * c);
         }
         const float stored = p.lo > 0 ? *scale : 0.0f;
 #pragma unroll

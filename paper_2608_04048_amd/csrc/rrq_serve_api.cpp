@@ -129,7 +129,7 @@ extern "C" int rrq_cache_attention_workspace(const rrq_cache *cache, const rrq_b
     *workspace_bytes = 0;
     if (batch->n_seqs == 0 || batch->n_tokens == 0) return RRQ_OK;
     *workspace_bytes = attend_bytes(cache, batch, n_heads,
-                                    attend_splits(*cache, *batch, n_heads));
+                                    attend_plan(*cache, *batch, n_heads).splits);
     return RRQ_OK;
 }
 
@@ -164,7 +164,11 @@ extern "C" int rrq_cache_attention(const rrq_cache *cache, const rrq_batch *batc
     a.causal = causal;
     a.q_bf16 = q_dtype == RRQ_BF16;
     a.out_bf16 = out_dtype == RRQ_BF16;
-    a.n_splits = attend_splits(*cache, *batch, n_heads);
+    const AttendPlan plan = attend_plan(*cache, *batch, n_heads);
+    a.n_splits = plan.splits;
+    a.target = plan.target;
+    a.min_tiles = plan.min_tiles;
+    a.lds_rows = plan.lds_rows;
     const size_t need = attend_bytes(cache, batch, n_heads, a.n_splits);
     if (need > 0) {
         if (!workspace) return RRQ_ERR_NULL;
@@ -173,7 +177,7 @@ extern "C" int rrq_cache_attention(const rrq_cache *cache, const rrq_batch *batc
         a.part_o = static_cast<float *>(workspace);
         a.part_ml = a.part_o + (size_t)a.n_splits * batch->n_tokens * n_heads * cache->head_dim;
     }
-    return status(launch_attend(a, stream));
+    return status(launch_attend(a, plan, stream));
 }
 
 namespace {

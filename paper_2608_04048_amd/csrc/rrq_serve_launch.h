@@ -42,10 +42,25 @@ struct CacheRead {
 hipError_t launch_cache_read(const CacheRead &a, bool bf16, hipStream_t stream);
 
 // Attention. Rows of a sequence and kv head are (token, query head of the
-// group): row r is token r / ratio, head kv * ratio + r % ratio. Row tiles of
-// kAttendRows rows; at most offsets[b + 1] * ratio / R - offsets[b] * ratio / R
-// + 1 tiles hold a sequence's rows.
-constexpr int kAttendRows = 16;
+// group): row r is token r / ratio, head kv * ratio + r % ratio. Two forms: few
+// rows a sequence (row tiles of 16, rrq_attention.hip) and many (row tiles of
+// 128, rrq_attention_rows.hip). At most offsets[b + 1] * ratio / R - offsets[b]
+// * ratio / R + 1 tiles of R rows hold a sequence's rows.
+constexpr int kFewTile = 16, kRowsTile = 128;
+// Rows a sequence (on average) up to which the few-row form serves a call.
+constexpr int64_t kFewMaxRows = 32;
+inline int64_t attend_row_tiles(const rrq_batch &b, int ratio, int tile)
+{
+    return b.n_tokens * ratio / tile + b.n_seqs;
+}
+// How a call is served: the form; the key ranges a row tile is split into at
+// most, of min_tiles 64-key tiles at least, about target workgroups in all;
+// waves a workgroup and rows a tile of the few-row form.
+struct AttendPlan {
+    bool rows_form;
+    int splits, target, min_tiles, waves, lds_rows;
+};
+AttendPlan attend_plan(const rrq_cache &c, const rrq_batch &b, int n_heads);
 struct Attend {
     rrq_cache cache;
     rrq_batch batch;
@@ -56,15 +71,11 @@ struct Attend {
     float *part_ml;     // [n_splits][n_tokens][n_heads][2]
     int64_t window;     // 0: none
     float scale;
-    int32_t n_heads, ratio, causal, q_bf16, out_bf16, n_splits;
+    int32_t n_heads, ratio, causal, q_bf16, out_bf16;
+    int32_t n_splits, target, min_tiles, lds_rows;
 };
-// Key ranges a row tile is split into at most.
-int attend_splits(const rrq_cache &c, const rrq_batch &b, int n_heads);
-inline int64_t attend_row_tiles(const rrq_batch &b, int ratio)
-{
-    return b.n_tokens * ratio / kAttendRows + b.n_seqs;
-}
-hipError_t launch_attend(const Attend &a, hipStream_t stream);
+hipError_t launch_attend(const Attend &a, const AttendPlan &p, hipStream_t stream);
+hipError_t launch_attend_rows(const Attend &a, hipStream_t stream);
 
 struct Logprobs {
     const void *logits;
