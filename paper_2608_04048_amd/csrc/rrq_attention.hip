@@ -354,9 +354,9 @@ AttendPlan attend_plan(const rrq_cache &c, const rrq_batch &b, int n_heads)
         p.waves = many_waves(c.head_dim);
         return p;
     }
-    p.target = p.rows_form ? 1024 : 2048;
-    p.min_tiles = p.rows_form ? 8 : 8;
-    if (units >= p.target) return p;
+    p.target = p.rows_form ? 512 : 2048;
+    p.min_tiles = 8;
+    if (units >= (p.rows_form ? kServeCus : p.target)) return p;
     const int64_t most = (cap + p.min_tiles * kTileKeys - 1) / (p.min_tiles * kTileKeys);
     int64_t n = 4 * p.target / units;
     n = n > most ? most : n;

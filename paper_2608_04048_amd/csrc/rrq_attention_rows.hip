@@ -18,19 +18,30 @@
 //
 // The running maximum m moves only when a tile's exceeds it by 8 (weights
 // then grow to 2^8 at most): most tiles skip the output's rescaling.
-#include <type_traits>
-
 #include "rrq_attention.h"
 
 namespace rrq_detail {
 namespace {
 
-constexpr int kKeys = kTileKeys;
 constexpr float kSlack = 8.0f;
 // Weights carry a factor of 2^6: with the slack's 2^8 they reach 2^14 in
 // binary16, and its normal range ends at 2^-20 of a row's largest weight.
 
+// Passes a NaN on, unlike fmaxf, which needs its operands quieted first.
+__device__ __forceinline__ float maximum(float a, float b)
+{
+    return __builtin_elementwise_maximum(a, b);
+}
+
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// The larger of a lane's value and that of the lane 32 away.
+__device__ __forceinline__ float other_half_max(float x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                    false);
+    return maximum(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
 
 // Lane i's value in every lane.
 __device__ __forceinline__ float lane_value(float x, int i)
@@ -38,15 +49,28 @@ __device__ __forceinline__ float lane_value(float x, int i)
     return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), i));
 }
 
-template <int D, int CODE>
-__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_rows_kernel(Attend a)
+// A key row in LDS: the first halves of its 16-channel pieces, then the second
+// halves (so that a wave's 16-byte writes fall in different banks). First
+// channel of the 16-byte slot.
+template <int D>
+__device__ __forceinline__ int channel_of(int slot)
+{
+    constexpr int KP = D / 16;
+    return slot < KP ? 16 * slot : 16 * (slot - KP) + 8;
+}
+
+// KEYS: keys of a tile, 32 or 64.
+template <int D, int CODE, int KEYS>
+__global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
 {
     constexpr int KROW = D * 2 + 16;        // LDS bytes of a key row: 16 more than a
-    constexpr int VROW = kKeys * 2 + 16;    // multiple of 128, so 8 rows span all banks
-    constexpr int KB = kKeys * KROW, VB = D * VROW;
-    constexpr int KT = kKeys * D / 16 / 256;    // 16-code pieces a thread stages
-    constexpr int ND = D / 32, NK = D / 16;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * (KB + VB)];
+    constexpr int VROW = KEYS * 2 + 16;    // multiple of 128, so 8 rows span all banks
+    constexpr int KB = KEYS * KROW, VB = D * VROW;
+    constexpr int BUF = KB + VB + 64;       // and the scales of its runs
+    constexpr int R = kRowsTile;
+    constexpr int KT = KEYS * D / 16 / 256;    // 16-code pieces a thread stages
+    constexpr int ND = D / 32, NK = D / 16, NH = KEYS / 32, RUNS = KEYS / 16;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * BUF];
 
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const int col = lane & 31, hb = lane >> 5;
@@ -56,7 +80,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_rows_kernel(Atte
     // most keys, come first
     const int kvh = blockIdx.x % H;
     RowTile r;
-    if (!find_rows<kRowsTile>(a, gridDim.x / H - 1 - blockIdx.x / H, r)) return;
+    if (!find_rows<R>(a, gridDim.x / H - 1 - blockIdx.x / H, r)) return;
 
     const int64_t row = r.row0 + 32 * wave + col;
     const bool live = row < r.n_rows;
@@ -64,21 +88,24 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_rows_kernel(Atte
     const int head = kvh * a.ratio + (int)((live ? row : r.n_rows - 1) % a.ratio);
     int lo, hi, lo_any, hi_any, lo_all, hi_all;
     row_keys(a, r, token, lo, hi);
-    tile_keys<kRowsTile>(a, r, lo_any, hi_any, lo_all, hi_all);
+    tile_keys<R>(a, r, lo_any, hi_any, lo_all, hi_all);
     int tb, te;
-    split_tiles<kRowsTile>(a, lo_any, hi_any, blockIdx.y, tb, te);
+    split_tiles<R>(a, lo_any, hi_any, blockIdx.y, tb, te);
+    tb *= kTileKeys / KEYS;                 // to tiles of KEYS
+    te *= kTileKeys / KEYS;
     const int32_t *table = a.batch.page_table + r.seq * a.batch.table_stride;
 
-    // queries: lane (col, hb) holds channels 16 j + 8 hb .. + 7 of its row
+    // queries: lane (col, hb) holds 8 channels of its row a product, in the
+    // order in which key rows stand in LDS
     f16x8 q[NK];
     float qf;
     {
         float x[NK][8];
         float amax = 0.0f;
-        const int64_t at = (r.o0 + token) * a.q_token + head * a.q_head + 8 * hb;
+        const int64_t at = (r.o0 + token) * a.q_token + head * a.q_head;
 #pragma unroll
         for (int j = 0; j < NK; ++j) {
-            load_query<8>(a, at + 16 * j, x[j]);
+            load_query<8>(a, at + channel_of<D>(2 * j + hb), x[j]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) amax = fmaxf(amax, fabsf(x[j][e]));
         }
@@ -93,25 +120,26 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_rows_kernel(Atte
 
     // Staging. Keys: thread t takes 16-code piece t % KP of key rows t / KP +
     // KSTEP i; a wave's rows lie in one run, so their page is wave-uniform.
-    // Values: run t % 4 of channel t / 4 + 64 i. Lane % 4 is the run whose page
-    // and scales a lane looks up.
-    constexpr int KP = D / 16, KSTEP = 256 / KP;
+    // Values: run t % RUNS of channel t / RUNS + VSTEP i. Lane % RUNS is the run
+    // whose page and scales a lane looks up.
+    constexpr int KP = D / 16, KSTEP = 256 / KP, VSTEP = 256 / RUNS;
     const int shift = __builtin_ctz(P);
     const int64_t head_bytes = (int64_t)P * D;
-    const int krow = t / KP, vrun = t & 3;
+    const int krow = t / KP, vrun = t % RUNS;
     u32x4v kw[KT], vw[KT];
-    int page = -1;                      // of the tile after the one in registers
-    float ksr, vsr;                     // of the tile in registers: its scales (0: absent)
+    int page;                           // of the tile after the one in registers
+    float ksr, vsr;                     // of the tile in registers: its scales
     bool absent;                        // and whether the lane's run is absent
-    // Tiles past the last are the last again: staged, never used.
+    // Loads without a branch: tiles past the last are the last again (staged,
+    // never used), a run past the keys has the last key's page, an absent page
+    // is read as page 0.
     auto find_page = [&](int tile) {
-        const int key = (tile < te ? tile : te - 1) * kKeys + 16 * vrun;
-        page = -1;
-        if (key < hi_any && key + 16 > lo_any) page = table[key >> shift];
+        const int key = (tile < te ? tile : te - 1) * KEYS + 16 * vrun;
+        page = table[(key < hi_any ? key : hi_any - 1) >> shift];
     };
     auto load_tile = [&](int tile) {
-        const int key0 = (tile < te ? tile : te - 1) * kKeys;
-        absent = (uint32_t)page >= (uint64_t)a.cache.n_pages;
+        const int key0 = (tile < te ? tile : te - 1) * KEYS, run = key0 + 16 * vrun;
+        absent = run >= hi_any || run + 16 <= lo_any || (uint32_t)page >= (uint64_t)a.cache.n_pages;
         const int safe = absent ? 0 : page;
 #pragma unroll
         for (int i = 0; i < KT; ++i) {
@@ -123,17 +151,17 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_rows_kernel(Atte
         }
         const int64_t block = (int64_t)safe * H + kvh;
         const uint8_t *src = a.cache.v_codes + block * head_bytes +
-                             (uint32_t)((t / 4) * P + ((key0 + 16 * vrun) & (P - 1)));
+                             (uint32_t)((t / RUNS) * P + ((key0 + 16 * vrun) & (P - 1)));
 #pragma unroll
         for (int i = 0; i < KT; ++i)
-            vw[i] = *reinterpret_cast<const u32x4v *>(src + 64 * i * P);
-        ksr = absent ? 0.0f : a.cache.k_scales[block];
-        vsr = absent ? 0.0f : a.cache.v_scales[block];
+            vw[i] = *reinterpret_cast<const u32x4v *>(src + VSTEP * i * P);
+        ksr = a.cache.k_scales[block];
+        vsr = a.cache.v_scales[block];
     };
     // Values of keys that no row sees may be left over from another use of the
     // page (not numbers, even): cleared.
     auto clear_unseen = [&](int tile) {
-        const int run = (tile < te ? tile : te - 1) * kKeys + 16 * vrun;
+        const int run = (tile < te ? tile : te - 1) * KEYS + 16 * vrun;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
             uint32_t keep = 0;
@@ -149,20 +177,31 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_rows_kernel(Atte
     auto store_tile = [&](uint8_t *buf) {
 #pragma unroll
         for (int i = 0; i < KT; ++i) {
-            uint8_t *at = buf + (krow + KSTEP * i) * KROW + 32 * (t % KP);
+            uint8_t *at = buf + (krow + KSTEP * i) * KROW + 16 * (t % KP);
             *reinterpret_cast<f16x8 *>(at) = codes_f16<CODE>(kw[i][0], kw[i][1]);
-            *reinterpret_cast<f16x8 *>(at + 16) = codes_f16<CODE>(kw[i][2], kw[i][3]);
+            *reinterpret_cast<f16x8 *>(at + D) = codes_f16<CODE>(kw[i][2], kw[i][3]);
         }
 #pragma unroll
         for (int i = 0; i < KT; ++i) {
-            uint8_t *at = buf + KB + (t / 4 + 64 * i) * VROW + 32 * vrun;
+            uint8_t *at = buf + KB + (t / RUNS + VSTEP * i) * VROW + 32 * vrun;
             *reinterpret_cast<f16x8 *>(at) = codes_f16<CODE>(vw[i][0], vw[i][2]);
             *reinterpret_cast<f16x8 *>(at + 16) = codes_f16<CODE>(vw[i][1], vw[i][3]);
         }
+        // a value scale below 0 marks an absent run
+        if (t < RUNS)
+            *reinterpret_cast<f32x2 *>(buf + KB + VB + 8 * t) =
+                f32x2{absent ? 0.0f : ksr, absent ? -1.0f : vsr};
     };
     // tiles whose keys not every row sees
     auto at_edge = [&](int tile) {
-        return tile * kKeys < lo_all || tile * kKeys + kKeys > hi_all;
+        return tile * KEYS < lo_all || tile * KEYS + KEYS > hi_all;
+    };
+
+    // LDS accesses done; global loads stay in flight.
+    auto barrier = [&] {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
     };
 
     float m = -kInf, l = 0.0f, vref = 0.0f;
@@ -172,118 +211,112 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void attend_rows_kernel(Atte
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[n][e] = 0.0f;
 
-    float kst = 0.0f, vst = 0.0f;       // scales of the tile in LDS
-    uint32_t gone = 0;                  // its absent runs
     if (tb < te) {
         find_page(tb);
         load_tile(tb);
         find_page(tb + 1);
         clear_unseen(tb);
-        store_tile(lds + (tb & 1) * (KB + VB));
-        kst = ksr;
-        vst = vsr;
-        gone = (uint32_t)__ballot(absent) & 15u;
+        store_tile(lds + (tb & 1) * BUF);
         load_tile(tb + 1);
         find_page(tb + 2);
-        __syncthreads();
+        barrier();
     }
     for (int tile = tb; tile < te; ++tile) {
-        const uint8_t *buf = lds + (tile & 1) * (KB + VB);
-        const uint32_t next_gone = (uint32_t)__ballot(absent) & 15u;
-        if (at_edge(tile + 1) || next_gone) clear_unseen(tile + 1);
+        const uint8_t *buf = lds + (tile & 1) * BUF;
+        if (at_edge(tile + 1) || __any(absent)) clear_unseen(tile + 1);
+        // scales of run lane % RUNS, and the tile's absent runs
+        const f32x2 scales = *reinterpret_cast<const f32x2 *>(buf + KB + VB + 8 * vrun);
+        const float kst = scales[0], vst = scales[1];
+        const uint32_t gone = (uint32_t)__ballot(vst < 0.0f) & ((1u << RUNS) - 1);
 
-        f32x16 s[2];
+        f32x16 s[NH];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < NH; ++h)
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[h][e] = 0.0f;
 #pragma unroll
-            for (int j = 0; j < NK; ++j) {
+        for (int j = 0; j < NK; ++j)
+#pragma unroll
+            for (int h = 0; h < NH; ++h) {
                 const f16x8 k = *reinterpret_cast<const f16x8 *>(
                     buf + (32 * h + col) * KROW + 32 * j + 16 * hb);
                 s[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[j], s[h], 0, 0, 0);
             }
-        }
-        store_tile(lds + ((tile + 1) & 1) * (KB + VB));
-        const float next_ks = ksr, next_vs = vsr;
+        store_tile(lds + ((tile + 1) & 1) * BUF);
         load_tile(tile + 2);
         find_page(tile + 3);
 
-        f16x8 p[4];
-        // c: factor of a run's products; masked: -inf stands for a key the row
-        // does not see
-        auto softmax = [&](auto masked) {
-            float tmax = -kInf, c[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float x = s[i >> 1][8 * (i & 1)];
-#pragma unroll
-                for (int e = 1; e < 8; ++e) x = fmaxf(x, s[i >> 1][8 * (i & 1) + e]);
-                c[i] = lane_value(kst, i) * qf;
-                // a run without a visible key: -inf stays, even times 0
-                tmax = fmaxf(tmax, masked && x == -kInf ? -kInf : x * c[i]);
-            }
-            tmax = fmaxf(tmax, __shfl_xor(tmax, 32));
-            const float vmax = fmaxf(fmaxf(lane_value(vst, 0), lane_value(vst, 1)),
-                                     fmaxf(lane_value(vst, 2), lane_value(vst, 3)));
-            if (__any(tmax > m + kSlack) || vmax > vref) {
-                const float mn = fmaxf(m, tmax);
-                const float alpha = mn == -kInf ? 0.0f : exp2_fast(m - mn);
-                m = mn;
-                l *= alpha;
-                const float vn = fmaxf(vref, vmax);
-                const float oa = vn > 0.0f ? alpha * (vref / vn) : 0.0f;
-                vref = vn;
-#pragma unroll
-                for (int n = 0; n < ND; ++n) o[n] *= oa;
-            }
-            const float ms = (m == -kInf ? 0.0f : m) - 6.0f;    // - 6: the weights' factor
-            // vref / vs of the lane's run, and its log2. A block of zeros may
-            // take any scale: vref's keeps w at the weight. Past 2^100 w is 0
-            // in binary16 for any factor.
-            const float backs =
-                vst > 0.0f ? fminf(vref * __builtin_amdgcn_rcpf(vst), 0x1p100f) : 1.0f;
-            const float lbacks = __builtin_amdgcn_logf(backs);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float back = lane_value(backs, i), sub = ms + lane_value(lbacks, i);
-                float sum = 0.0f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float x = s[i >> 1][8 * (i & 1) + e];
-                    float w = exp2_fast(__builtin_fmaf(x, c[i], -sub));
-                    if (masked) w = x == -kInf ? 0.0f : w;
-                    sum += w;
-                    p[i][e] = (_Float16)w;
-                }
-                l += sum * back;
-            }
-        };
         if (at_edge(tile) || gone) {
+            // -inf stands for a key that the row does not see: its weight is
+            // exp2(-inf) = 0
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < NH; ++h)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int key = tile * kKeys + 32 * h + 8 * (e >> 2) + 4 * hb + (e & 3);
+                    const int key = tile * KEYS + 32 * h + 8 * (e >> 2) + 4 * hb + (e & 3);
                     if (key < lo || key >= hi || ((gone >> (2 * h + (e >> 3))) & 1))
                         s[h][e] = -kInf;
                 }
-            softmax(std::true_type{});
-        } else {
-            softmax(std::false_type{});
+        }
+        // c: factor of a run's products. 0 (a block of zeros) becomes the least
+        // number, which leaves -inf as it is.
+        float tmax = -kInf, c[RUNS];
+#pragma unroll
+        for (int i = 0; i < RUNS; ++i) {
+            c[i] = lane_value(kst, i) * qf;
+            if (c[i] == 0.0f) c[i] = 0x1p-126f;
+            float x = s[i >> 1][8 * (i & 1)];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) x = maximum(x, s[i >> 1][8 * (i & 1) + e]);
+            tmax = maximum(tmax, x * c[i]);
+        }
+        tmax = other_half_max(tmax);
+        float vmax = lane_value(vst, 0);
+#pragma unroll
+        for (int i = 1; i < RUNS; ++i) vmax = maximum(vmax, lane_value(vst, i));
+        if (__any(tmax > m + kSlack) || vmax > vref) {
+            const float mn = fmaxf(m, tmax);
+            const float alpha = mn == -kInf ? 0.0f : exp2_fast(m - mn);
+            m = mn;
+            l *= alpha;
+            const float vn = fmaxf(vref, vmax);
+            const float oa = vn > 0.0f ? alpha * (vref / vn) : 0.0f;
+            vref = vn;
+#pragma unroll
+            for (int n = 0; n < ND; ++n) o[n] *= oa;
+        }
+        const float ms = (m == -kInf ? 0.0f : m) - 6.0f;    // - 6: the weights' factor
+        // vref / vs of the lane's run, and its log2. A block of zeros may take
+        // any scale: vref's keeps w at the weight. Past 2^100 w is 0 in
+        // binary16 for any factor.
+        const float backs = vst > 0.0f ? fminf(vref * __builtin_amdgcn_rcpf(vst), 0x1p100f) : 1.0f;
+        const float lbacks = __builtin_amdgcn_logf(backs);
+        f16x8 p[RUNS];
+#pragma unroll
+        for (int i = 0; i < RUNS; ++i) {
+            const float back = lane_value(backs, i), sub = ms + lane_value(lbacks, i);
+            float sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                p[i][e] = (_Float16)exp2_fast(
+                    __builtin_fmaf(s[i >> 1][8 * (i & 1) + e], c[i], -sub));
+            // the rounded weights, as the second product takes them
+            const f16x2 ones = {(_Float16)1.0f, (_Float16)1.0f};
+#pragma unroll
+            for (int e = 0; e < 8; e += 2)
+                sum = __builtin_amdgcn_fdot2(f16x2{p[i][e], p[i][e + 1]}, ones, sum, false);
+            l += sum * back;
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < RUNS; ++i)
 #pragma unroll
             for (int n = 0; n < ND; ++n) {
                 const f16x8 v = *reinterpret_cast<const f16x8 *>(
                     buf + KB + (32 * n + col) * VROW + 32 * i + 16 * hb);
                 o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[i], o[n], 0, 0, 0);
             }
-        kst = next_ks;
-        vst = next_vs;
-        gone = next_gone;
-        __syncthreads();
+        //SCHED
+        barrier();
     }
 
     // both l and o carry the weights' factor
@@ -327,8 +360,9 @@ hipError_t rows_dim(const Attend &a, hipStream_t stream)
 {
     const dim3 grid((unsigned)(attend_row_tiles(a.batch, a.ratio, kRowsTile) *
                                a.cache.n_kv_heads), a.n_splits);
-    auto kernel = a.cache.code_type == RRQ_CODE_INT8 ? attend_rows_kernel<D, RRQ_CODE_INT8>
-                                                     : attend_rows_kernel<D, RRQ_CODE_FP8>;
+    constexpr int KEYS = D == 256 ? 32 : 64;
+    auto kernel = a.cache.code_type == RRQ_CODE_INT8 ? attend_rows_kernel<D, RRQ_CODE_INT8, KEYS>
+                                                     : attend_rows_kernel<D, RRQ_CODE_FP8, KEYS>;
     kernel<<<grid, 256, 0, stream>>>(a);
     return hipGetLastError();
 }
