@@ -21,42 +21,53 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 // rows (tokens x ratio) from dense row o0 on, its first token at position
 // start of len.
 struct RowTile {
-    int64_t seq, row0;
-    int64_t o0, n_rows;
-    int64_t len, start;
+    int seq, row0;
+    int o0, n_rows;
+    int len, start;
 };
 
-__device__ __forceinline__ int64_t clamp_length(const Attend &a, int64_t len)
+__device__ __forceinline__ int clamp_length(const Attend &a, int len)
 {
     int64_t cap = a.batch.max_pages * a.cache.page_size;
     if (cap > kMaxPositions) cap = kMaxPositions;
-    return len < 0 ? 0 : (len > cap ? cap : len);
+    return len < 0 ? 0 : (len > cap ? (int)cap : len);
 }
 
 // The rows of tile slot u, tiles of R rows.
 template <int R>
-__device__ __forceinline__ bool find_rows(const Attend &a, int64_t u, RowTile &r)
+__device__ __forceinline__ bool find_rows(const Attend &a, int u, RowTile &r)
 {
-    const int64_t s = find_sequence(a.batch, u, a.ratio, R, 1);
+    constexpr int shift = __builtin_ctz(R);
+    const int s = find_sequence(a.batch, u, a.ratio, shift, 1);
     r.seq = s;
     r.o0 = clamp_row(a.batch, s);
-    const int64_t n = clamp_row(a.batch, s + 1) - r.o0;
-    r.row0 = (u - (r.o0 * a.ratio / R + s)) * R;
+    const int n = clamp_row(a.batch, s + 1) - r.o0;
+    const int len = a.batch.lengths[s];
+    r.row0 = (u - ((r.o0 * a.ratio >> shift) + s)) * R;
     r.n_rows = n * a.ratio;
     if (n <= 0 || r.row0 < 0 || r.row0 >= r.n_rows) return false;   // < 0: before the first sequence
-    const int64_t len = a.batch.lengths[s];
     r.start = len - n;
     r.len = clamp_length(a, len);
     return true;
 }
 
+// A row's token and query head within the kv head's group.
+struct RowPlace {
+    int token, member;
+};
+__device__ __forceinline__ RowPlace place_of(const Attend &a, int row)
+{
+    const uint32_t token = (uint32_t)row / (uint32_t)a.ratio;
+    return RowPlace{(int)token, row - (int)token * a.ratio};
+}
+
 // Keys row token i sees: [lo, hi).
-__device__ __forceinline__ void row_keys(const Attend &a, const RowTile &r, int64_t i, int &lo,
+__device__ __forceinline__ void row_keys(const Attend &a, const RowTile &r, int i, int &lo,
                                          int &hi)
 {
-    const int64_t pos = r.start + i;
-    int64_t h = a.causal && pos + 1 < r.len ? pos + 1 : r.len;
-    int64_t l = a.window > 0 && pos + 1 > a.window ? pos + 1 - a.window : 0;
+    const int64_t end = (int64_t)r.start + i + 1;       // one past the token's position
+    int64_t h = a.causal && end < r.len ? end : r.len;
+    int64_t l = a.window > 0 && end > a.window ? end - a.window : 0;
     if (h < 0) h = 0;
     if (l > h) l = h;
     lo = (int)l;
@@ -69,9 +80,9 @@ template <int R>
 __device__ __forceinline__ void tile_keys(const Attend &a, const RowTile &r, int &lo_any,
                                           int &hi_any, int &lo_all, int &hi_all)
 {
-    const int64_t end = r.row0 + R < r.n_rows ? r.row0 + R : r.n_rows;
-    row_keys(a, r, r.row0 / a.ratio, lo_any, hi_all);
-    row_keys(a, r, (end - 1) / a.ratio, lo_all, hi_any);
+    const int end = r.row0 + R < r.n_rows ? r.row0 + R : r.n_rows;
+    row_keys(a, r, place_of(a, r.row0).token, lo_any, hi_all);
+    row_keys(a, r, place_of(a, end - 1).token, lo_all, hi_any);
 }
 
 // Key tiles of the whole batch, times the row tiles that read them (one kv
@@ -80,12 +91,12 @@ template <int R>
 __device__ __forceinline__ int64_t batch_tiles(const Attend &a)
 {
     int64_t sum = 0;
-    for (int64_t s = threadIdx.x & 63; s < a.batch.n_seqs; s += 64) {
-        const int64_t n = clamp_row(a.batch, s + 1) - clamp_row(a.batch, s);
+    for (int s = threadIdx.x & 63; s < a.batch.n_seqs; s += 64) {
+        const int n = clamp_row(a.batch, s + 1) - clamp_row(a.batch, s);
         if (n <= 0) continue;
         int64_t keys = clamp_length(a, a.batch.lengths[s]);
         if (a.window > 0 && keys > a.window + n) keys = a.window + n;
-        sum += (keys + kTileKeys - 1) / kTileKeys * ((n * a.ratio + R - 1) / R);
+        sum += ((keys + kTileKeys - 1) >> 6) * ((n * a.ratio + R - 1) / R);
     }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
@@ -103,9 +114,12 @@ __device__ __forceinline__ void split_tiles(const Attend &a, int lo, int hi, int
     const int tiles = hi > lo ? (hi + kTileKeys - 1) / kTileKeys - t0 : 0;
     int per = tiles;
     if (a.n_splits > 1) {
-        const int64_t even = (batch_tiles<R>(a) * a.cache.n_kv_heads + a.target - 1) / a.target;
-        per = (tiles + a.n_splits - 1) / a.n_splits;
-        per = per < even ? (int)even : per;
+        // (the mean to a rounding of binary32 will do)
+        const float even = (float)batch_tiles<R>(a) * (float)a.cache.n_kv_heads / (float)a.target;
+        per = (int)((uint32_t)(tiles + a.n_splits - 1) / (uint32_t)a.n_splits);
+        const int most = 1 << 26;
+        const int want = even < (float)most ? (int)even + 1 : most;
+        per = per < want ? want : per;
         per = per < a.min_tiles ? a.min_tiles : per;
     }
     tb = split * per < tiles ? t0 + split * per : t0 + tiles;

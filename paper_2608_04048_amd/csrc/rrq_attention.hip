@@ -66,16 +66,17 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
     if (!find_rows<kFewTile>(a, blockIdx.x, r)) return;
 
     // this lane's row
-    const int64_t row = r.row0 + col;
-    const bool live = row < r.n_rows;
-    const int64_t token = (live ? row : r.n_rows - 1) / a.ratio;
-    const int head = kvh * a.ratio + (int)((live ? row : r.n_rows - 1) % a.ratio);
+    const int row = r.row0 + col;
+    const RowPlace place = place_of(a, row < r.n_rows ? row : r.n_rows - 1);
+    const int64_t token = place.token;
+    const int head = kvh * a.ratio + place.member;
     int lo, hi, lo_any, hi_any, lo_all, hi_all, tb, te;
-    row_keys(a, r, token, lo, hi);
+    row_keys(a, r, place.token, lo, hi);
     tile_keys<kFewTile>(a, r, lo_any, hi_any, lo_all, hi_all);
     split_tiles<kFewTile>(a, lo_any, hi_any, split, tb, te);
 
     const int P = a.cache.page_size, H = a.cache.n_kv_heads;
+    const int shift = __builtin_ctz(P);
     const int32_t *table = a.batch.page_table + r.seq * a.batch.table_stride;
 
     // Queries: lane (col, g) holds channels 64 j + 16 g .. + 15 of its row.
@@ -108,7 +109,7 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
 
     // page number of the run of 16 keys at `key`, -1 if no row sees one of them
     auto page_of = [&](int key) {
-        return key < hi_any && key + 16 > lo_any ? table[key / P] : -1;
+        return key < hi_any && key + 16 > lo_any ? table[key >> shift] : -1;
     };
     // of the run this lane loads keys of (matrix rows col: run col / 4) and of
     // the run it owns (g), one tile ahead
@@ -124,8 +125,8 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
         const int64_t kb = kpage >= 0 && kpage < a.cache.n_pages ? kpage : 0;
         const int64_t ob = (int64_t)(there ? opage : 0) * H + kvh;
         const uint8_t *kc = a.cache.k_codes + (kb * H + kvh) * P * D +
-                            (krun % P + (col & 3)) * D + 16 * g;
-        const uint8_t *vc = a.cache.v_codes + ob * P * D + (int64_t)col * P + orun % P;
+                            ((krun & (P - 1)) + (col & 3)) * D + 16 * g;
+        const uint8_t *vc = a.cache.v_codes + ob * P * D + (int64_t)(col * P + (orun & (P - 1)));
         u32x4v kw[4][KL], vw[ND];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -229,7 +230,7 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
     }
     __syncthreads();
     // 4 channels a thread
-    const int rows = r.n_rows - r.row0 < kFewTile ? (int)(r.n_rows - r.row0) : kFewTile;
+    const int rows = r.n_rows - r.row0 < kFewTile ? r.n_rows - r.row0 : kFewTile;
     for (int i = threadIdx.x; i < rows * (D / 4); i += 64 * NW) {
         const int orow = i / (D / 4), d = i % (D / 4) * 4;
         float mm = -kInf, ll = 0.0f;
@@ -244,8 +245,9 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
             ll += f * lds_ml[at * 2 + 1];
             y += f * *reinterpret_cast<const f32x4 *>(lds + at * (D + 4) + d);
         }
-        const int64_t otok = r.o0 + (r.row0 + orow) / a.ratio;
-        const int64_t at = otok * a.n_heads + kvh * a.ratio + (r.row0 + orow) % a.ratio;
+        const RowPlace place = place_of(a, r.row0 + orow);
+        const int64_t at = (int64_t)(r.o0 + place.token) * a.n_heads + kvh * a.ratio +
+                           place.member;
         if (a.n_splits > 1) {
             const int64_t part = (int64_t)split * a.batch.n_tokens * a.n_heads + at;
             if (d == 0) {
@@ -264,21 +266,22 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
     }
 }
 
-// Joins the key ranges of a row: one wave a (token, head). Lane s holds range
-// s's maximum and sum, so the factors cost one load; the outputs of the ranges
-// up to the last with a sum (all written) are then read without a branch.
-template <int D>
-__global__ __launch_bounds__(256) void attend_join_kernel(Attend a)
+// Joins the key ranges of a row (token, head): one workgroup of W waves a row,
+// wave w takes ranges w, w + W, ... Lane s holds range s's maximum and sum, so
+// the factors cost one load. The ranges up to the last with a sum were all
+// written; they are read four at a time, those past it as the last, times 0.
+template <int D, int W>
+__global__ __launch_bounds__(64 * W) void attend_join_kernel(Attend a)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t rows = a.batch.n_tokens * a.n_heads;
-    const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (at >= rows) return;
-    const int64_t token = at / a.n_heads;
-    if (token < clamp_row(a.batch, 0) || token >= clamp_row(a.batch, a.batch.n_seqs)) return;
+    constexpr int N = D / 64;
+    __shared__ float lds[W][D];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t rows = a.batch.n_tokens * a.n_heads, at = blockIdx.x;
     f32x2 ml = {-kInf, 0.0f};
     if (lane < a.n_splits)
         ml = *reinterpret_cast<const f32x2 *>(a.part_ml + 2 * (lane * rows + at));
+    const int token = (int)(blockIdx.x / (uint32_t)a.n_heads);
+    if (token < clamp_row(a.batch, 0) || token >= clamp_row(a.batch, (int)a.batch.n_seqs)) return;
     float m = ml[0];
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
@@ -287,20 +290,39 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Attend a)
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
     const uint64_t has = __ballot(ml[1] != 0.0f);
-    const int used = has ? 64 - __builtin_clzll(has) : 0;
-    float y[D / 64] = {};
-    const float *src = a.part_o + at * D + lane * (D / 64);
-#pragma unroll 8
-    for (int s = 0; s < used; ++s) {
-        const float fs = __shfl(f, s);
+    const int last = has ? 63 - __builtin_clzll(has) : -1;
+    float y[N] = {};
+    const float *src = a.part_o + at * D + lane * N;
+    for (int s = wave; s <= last; s += 4 * W) {
+        float x[4][N];
 #pragma unroll
-        for (int d = 0; d < D / 64; ++d) y[d] += fs * src[s * rows * D + d];
+        for (int i = 0; i < 4; ++i) {
+            const int r = s + i * W < last ? s + i * W : last;
+#pragma unroll
+            for (int d = 0; d < N; ++d) x[i][d] = src[r * rows * D + d];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float fs = s + i * W <= last ? __shfl(f, s + i * W) : 0.0f;
+#pragma unroll
+            for (int d = 0; d < N; ++d) y[d] += fs * x[i][d];
+        }
+    }
+    if (W > 1) {
+#pragma unroll
+        for (int d = 0; d < N; ++d) lds[wave][lane * N + d] = y[d];
+        __syncthreads();
+        if (wave > 0) return;
+#pragma unroll
+        for (int d = 0; d < N; ++d)
+#pragma unroll
+            for (int w = 1; w < W; ++w) y[d] += lds[w][lane * N + d];
     }
     const float norm = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-    for (int d = 0; d < D / 64; ++d) {
+    for (int d = 0; d < N; ++d) {
         const float v = y[d] * norm;
-        const int64_t i = at * D + lane * (D / 64) + d;
+        const int64_t i = at * D + lane * N + d;
         if (a.out_bf16)
             static_cast<uint16_t *>(a.out)[i] = (uint16_t)bf16_bits(v);
         else
@@ -331,8 +353,11 @@ hipError_t few_dim(const Attend &a, int waves, hipStream_t stream)
 template <int D>
 hipError_t join_dim(const Attend &a, hipStream_t stream)
 {
-    const int64_t rows = a.batch.n_tokens * a.n_heads;
-    attend_join_kernel<D><<<(unsigned)((rows + 3) / 4), 256, 0, stream>>>(a);
+    const unsigned rows = (unsigned)(a.batch.n_tokens * a.n_heads);
+    if (a.n_splits > 8)
+        attend_join_kernel<D, 4><<<rows, 256, 0, stream>>>(a);
+    else
+        attend_join_kernel<D, 1><<<rows, 64, 0, stream>>>(a);
     return hipGetLastError();
 }
 

@@ -82,12 +82,13 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
     RowTile r;
     if (!find_rows<R>(a, gridDim.x / H - 1 - blockIdx.x / H, r)) return;
 
-    const int64_t row = r.row0 + 32 * wave + col;
+    const int row = r.row0 + 32 * wave + col;
     const bool live = row < r.n_rows;
-    const int64_t token = (live ? row : r.n_rows - 1) / a.ratio;
-    const int head = kvh * a.ratio + (int)((live ? row : r.n_rows - 1) % a.ratio);
+    const RowPlace place = place_of(a, live ? row : r.n_rows - 1);
+    const int64_t token = place.token;
+    const int head = kvh * a.ratio + place.member;
     int lo, hi, lo_any, hi_any, lo_all, hi_all;
-    row_keys(a, r, token, lo, hi);
+    row_keys(a, r, place.token, lo, hi);
     tile_keys<R>(a, r, lo_any, hi_any, lo_all, hi_all);
     int tb, te;
     split_tiles<R>(a, lo_any, hi_any, blockIdx.y, tb, te);

@@ -24,22 +24,23 @@ struct PageSlot {
     }
 };
 
-__device__ __forceinline__ bool find_page(const rrq_cache &c, const rrq_batch &b, int64_t u,
+__device__ __forceinline__ bool find_page(const rrq_cache &c, const rrq_batch &b, int u,
                                           PageSlot &p)
 {
-    const int P = c.page_size;
-    const int64_t s = find_sequence(b, u, 1, P, 2);
-    const int64_t o0 = clamp_row(b, s), o1 = clamp_row(b, s + 1);
-    const int64_t len = b.lengths[s], start = len - (o1 - o0);
+    const int P = c.page_size, shift = __builtin_ctz(P);
+    const int s = find_sequence(b, u, 1, shift, 2);
+    const int o0 = clamp_row(b, s), o1 = clamp_row(b, s + 1), len = b.lengths[s];
     if (o1 <= o0 || len <= 0) return false;
-    const int64_t first = start < 0 ? 0 : start;      // rows before position 0 have no place
-    const int64_t slot = u - (o0 / P + 2 * s);         // < 0: before the first sequence
-    const int64_t j = first / P + slot;
-    if (slot < 0 || j * P >= len || j >= b.max_pages) return false;
+    const int start = len - (o1 - o0);
+    const int first = start < 0 ? 0 : start;        // rows before position 0 have no place
+    const int slot = u - ((o0 >> shift) + 2 * s);   // < 0: before the first sequence
+    const int64_t j = (first >> shift) + slot;
+    const int64_t at = j << shift;                  // the page's first position
+    if (slot < 0 || at >= len || j >= b.max_pages) return false;
     p.page = b.page_table[s * b.table_stride + j];
-    p.lo = j * P < first ? (int)(first - j * P) : 0;
-    p.hi = len - j * P < P ? (int)(len - j * P) : P;
-    p.row0 = o0 + j * P + p.lo - start;
+    p.lo = at < first ? (int)(first - at) : 0;
+    p.hi = len - at < P ? (int)(len - at) : P;
+    p.row0 = o0 + at + p.lo - start;
     return true;
 }
 

@@ -17,27 +17,30 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-__device__ __forceinline__ int64_t clamp_row(const rrq_batch &b, int64_t i)
+// Row numbers fit in 32 bits (n_tokens <= 2^26, times the query heads of a kv
+// head as well).
+__device__ __forceinline__ int clamp_row(const rrq_batch &b, int i)
 {
-    const int64_t o = b.offsets[i];
-    return o < 0 ? 0 : (o > b.n_tokens ? b.n_tokens : o);
+    const int o = b.offsets[i];
+    return o < 0 ? 0 : (o > b.n_tokens ? (int)b.n_tokens : o);
 }
 
 // The sequence that owns work slot u, where sequence b's slots start at
-// f(b) = offsets[b] * mul / div + extra * b. Every lane of the wave calls it;
-// each step compares 64 sequences at once, so up to 64 sequences cost one
+// f(b) = (offsets[b] * mul >> shift) + extra * b. Every lane of the wave calls
+// it; each step compares 64 sequences at once, so up to 64 sequences cost one
 // load.
-__device__ __forceinline__ int64_t find_sequence(const rrq_batch &b, int64_t u, int64_t mul,
-                                                 int64_t div, int64_t extra)
+__device__ __forceinline__ int find_sequence(const rrq_batch &b, int u, int mul, int shift,
+                                             int extra)
 {
     const int lane = threadIdx.x & 63;
-    int64_t lo = 0, n = b.n_seqs;
+    int lo = 0, n = (int)b.n_seqs;
     while (n > 1) {
-        const int64_t step = (n + 63) / 64;
-        const int64_t i = lane * step;
-        const bool below = i < n && (clamp_row(b, lo + i) * mul) / div + extra * (lo + i) <= u;
+        const int step = (n + 63) >> 6;
+        const int i = lane * step;
+        const bool below =
+            i < n && ((clamp_row(b, lo + i) * mul) >> shift) + extra * (lo + i) <= u;
         const int c = __popcll(__ballot(below));
-        const int64_t at = c > 0 ? (int64_t)(c - 1) * step : 0;
+        const int at = c > 0 ? (c - 1) * step : 0;
         lo += at;
         n = n - at < step ? n - at : step;
     }
