@@ -28,6 +28,7 @@ constexpr int kPerLane = 32;
 constexpr int kBlock = 64 * kPerLane;
 constexpr int kWaves = 4;
 constexpr int kBuffer = 128;            // keys a wave buffers
+constexpr int kSlots = kBuffer + 8;     // and what a cut pads them with
 typedef unsigned long long key_t;
 
 // Ascending order of floats as unsigned; NaN first.
@@ -90,18 +91,36 @@ struct Top {
     __device__ void cut()
     {
         const int lane = threadIdx.x & 63;
+        if (lane < 8) buf[count + lane] = 0;        // to whole groups of 8
         wave_sync();
         const key_t a = lane < count ? buf[lane] : 0;
-        const key_t b = lane + 64 < count ? buf[lane + 64] : 0;
-        int ra = 0, rb = 0;
-        for (int i = 0; i < count; ++i) {
-            const key_t o = buf[i];
-            ra += o > a;
-            rb += o > b;
+        int ra = 0;
+        if (count <= 64) {
+            for (int i = 0; i < count; i += 8) {
+                key_t o[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = buf[i + e];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) ra += o[e] > a;
+            }
+            wave_sync();
+        } else {
+            const key_t b = lane + 64 < count ? buf[lane + 64] : 0;
+            int rb = 0;
+            for (int i = 0; i < count; i += 8) {
+                key_t o[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = buf[i + e];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    ra += o[e] > a;
+                    rb += o[e] > b;
+                }
+            }
+            wave_sync();
+            if (lane + 64 < count && rb < n) buf[rb] = b;
         }
-        wave_sync();
         if (lane < count && ra < n) buf[ra] = a;
-        if (lane + 64 < count && rb < n) buf[rb] = b;
         wave_sync();
         if (count >= n) {
             count = n;
@@ -109,25 +128,37 @@ struct Top {
         }
     }
 
-    // Adds the lanes' keys that beat the floor (every lane calls it).
+    // A value below this cannot beat the floor (no number if anything can:
+    // nothing is below that).
+    __device__ float floor_value() const
+    {
+        const uint32_t o = (uint32_t)(floor >> 32);
+        return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
+    }
+
+    // Adds the keys of the lanes that have one (every lane calls it); there is
+    // room.
     __device__ void add(bool has, key_t k)
     {
-        const uint64_t who = __ballot(has && k > floor);
-        if (!who) return;
-        if (count > kBuffer - 64) cut();
-        // the cut may have raised the floor: some keys stay without need
+        const uint64_t who = __ballot(has);
         const int lane = threadIdx.x & 63;
         const int at = count + __popcll(who & ((1ull << lane) - 1));
         if ((who >> lane) & 1) buf[at] = k;
         count += __popcll(who);
     }
+    __device__ void add_or_cut(bool has, key_t k)
+    {
+        if (count > kBuffer - 64) cut();
+        add(has && k > floor, k);
+    }
 };
 
-// The n-th largest of the lanes' values (n <= 64).
+// A value that n lanes reach (n <= 64): the n-th largest in its upper 16 bits.
 __device__ __forceinline__ uint32_t nth_largest(uint32_t v, int n)
 {
     uint32_t r = 0;
-    for (int bit = 31; bit >= 0; --bit) {
+#pragma unroll
+    for (int bit = 31; bit >= 16; --bit) {
         const uint32_t c = r | (1u << bit);
         if (__popcll(__ballot(v >= c)) >= n) r = c;
     }
@@ -178,35 +209,35 @@ __device__ __forceinline__ void write_row(const Logprobs &a, int64_t row, const 
 }
 
 template <bool BF16>
-__global__ __launch_bounds__(64 * kWaves) void logprobs_kernel(Logprobs a)
+__global__ __launch_bounds__(64 * kWaves, 5) void logprobs_kernel(Logprobs a)
 {
-    __shared__ key_t lds_keys[kWaves][kBuffer];
+    __shared__ key_t lds_keys[kWaves][kSlots];
     __shared__ float lds_sums[kWaves][3];
     constexpr int VEC = BF16 ? 8 : 4;           // logits a load
     constexpr int NV = kPerLane / VEC;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t row = blockIdx.x / a.segments;
-    const int seg = blockIdx.x % a.segments;
+    const int64_t row = blockIdx.x / (uint32_t)a.segments;
+    const int seg = blockIdx.x % (uint32_t)a.segments;
     const char *x = static_cast<const char *>(a.logits) + row * a.row_stride * (BF16 ? 2 : 4);
     // parts of whole blocks, one a wave
-    const int64_t parts = (int64_t)a.segments * kWaves;
-    const int64_t blocks = (a.vocab + kBlock - 1) / kBlock;
-    const int64_t p = (int64_t)seg * kWaves + wave;
-    const int64_t b0 = blocks * p / parts, b1 = blocks * (p + 1) / parts;
+    const uint32_t vocab = (uint32_t)a.vocab;       // at most 2^30
+    const uint32_t parts = a.segments * kWaves, blocks = (vocab + kBlock - 1) / kBlock;
+    const uint32_t p = seg * kWaves + wave, each = blocks / parts, more = blocks % parts;
+    const uint32_t b0 = each * p + (p < more ? p : more), b1 = b0 + each + (p < more ? 1 : 0);
 
     Sums s = {-kInf, 0.0f, 0.0f};
     Top top = {lds_keys[wave], a.n_top, 0, 0};
-    for (int64_t b = b0; b < b1; ++b) {
-        const int64_t base = b * kBlock;
+    // rows may start at any multiple of their type: 16-byte loads without that
+    // alignment
+    struct __attribute__((packed, aligned(2))) Wide { uint32_t w[4]; };
+    for (uint32_t b = b0; b < b1; ++b) {
+        const uint32_t base = b * kBlock;
         float v[kPerLane];
-        if (base + kBlock <= a.vocab) {
-            // rows may start at any multiple of their type: 16-byte loads
-            // without that alignment
-            struct __attribute__((packed, aligned(2))) Wide { uint32_t w[4]; };
+        if (base + kBlock <= vocab) {
+            const char *src = x + ((int64_t)base + lane * VEC) * (BF16 ? 2 : 4);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const Wide w = *reinterpret_cast<const Wide *>(
-                    x + (base + (i * 64 + lane) * VEC) * (BF16 ? 2 : 4));
+                const Wide w = *reinterpret_cast<const Wide *>(src + i * 1024);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     if (BF16) {
@@ -220,8 +251,8 @@ __global__ __launch_bounds__(64 * kWaves) void logprobs_kernel(Logprobs a)
         } else {
 #pragma unroll
             for (int i = 0; i < kPerLane; ++i) {
-                const int64_t at = base + ((i / VEC) * 64 + lane) * VEC + i % VEC;
-                v[i] = at < a.vocab ? load_logit<BF16>(x, at) : -kInf;
+                const uint32_t at = base + ((i / VEC) * 64 + lane) * VEC + i % VEC;
+                v[i] = at < vocab ? load_logit<BF16>(x, at) : -kInf;
             }
         }
         float bm = -kInf;
@@ -237,33 +268,43 @@ __global__ __launch_bounds__(64 * kWaves) void logprobs_kernel(Logprobs a)
             // of 0 times infinity
             const float di = v[i] - ms, e = exp_of(di);
             l += e;
-            t += e * fmaxf(di, -1e30f);
+            t = __builtin_fmaf(e, fmaxf(di, -1e30f), t);
         }
         s.t = f * (s.t + d * s.l) + t;
         s.l = f * s.l + l;
         s.m = mn;
         if (a.n_top == 0) continue;
+        // (opaque, so that the slots' indices are formed where they are used
+        // and not kept in registers)
+        uint32_t at0 = base + lane * VEC;
+        asm volatile("" : "+v"(at0));
         // a later block has higher indices: an equal logit does not matter
         const uint32_t bo = ordered(bm);
         if (top.floor != 0 && !__any(bo > (uint32_t)(top.floor >> 32))) continue;
-        if (top.floor == 0 && top.count == 0) {
-            // The wave's first block: the n-th largest lane maximum is a
-            // floor that at least n logits reach. Lanes without a logit
-            // count as 0.
-            uint32_t lm = 0;
-#pragma unroll
-            for (int i = 0; i < kPerLane; ++i) {
-                const int64_t at = base + ((i / VEC) * 64 + lane) * VEC + i % VEC;
-                const uint32_t o = at < a.vocab ? ordered(v[i]) : 0;
-                lm = o > lm ? o : lm;
-            }
-            const uint32_t nth = nth_largest(lm, a.n_top);
-            if (nth > 0) top.floor = ((key_t)nth << 32) - 1;
-        }
+        // What n lanes' maxima reach is a floor that n logits reach. A maximum
+        // of -inf counts if it is a logit's, not just where the lane began.
+        const bool has = bm > -kInf || (at0 < vocab && v[0] == -kInf);
+        const uint32_t nth = nth_largest(has ? bo : 0, a.n_top);
+        const key_t least = ((key_t)nth << 32) - 1;
+        if (nth > 0 && least > top.floor) top.floor = least;
+        const float fv = top.floor_value();
+        int full = kPerLane;        // slot at which the buffer had no room
 #pragma unroll
         for (int i = 0; i < kPerLane; ++i) {
-            const int64_t at = base + ((i / VEC) * 64 + lane) * VEC + i % VEC;
-            top.add(at < a.vocab, make_key(ordered(v[i]), (uint32_t)at));
+            if (full < kPerLane || !__any(!(v[i] < fv))) continue;
+            if (top.count > kBuffer - 64) {
+                full = i;
+                continue;
+            }
+            const uint32_t at = at0 + (i / VEC) * 64 * VEC + i % VEC;
+            top.add(at < vocab && !(v[i] < fv), make_key(ordered(v[i]), at));
+        }
+        // rows in order, or many equal logits: slot by slot, read again
+#pragma unroll 1
+        for (int i = full; i < kPerLane; ++i) {
+            const uint32_t at = at0 + (i / VEC) * 64 * VEC + i % VEC;
+            const float y = at < vocab ? load_logit<BF16>(x, at) : 0.0f;
+            top.add_or_cut(at < vocab, make_key(ordered(y), at));
         }
         top.cut();
     }
@@ -280,9 +321,10 @@ __global__ __launch_bounds__(64 * kWaves) void logprobs_kernel(Logprobs a)
     for (int w = 1; w < kWaves; ++w)
         s = join(s, Sums{lds_sums[w][0], lds_sums[w][1], lds_sums[w][2]});
     if (a.n_top > 0) {
+#pragma unroll 1
         for (int w = 1; w < kWaves; ++w) {
             const key_t k = lane < a.n_top ? lds_keys[w][lane] : 0;
-            top.add(k != 0, k);
+            top.add_or_cut(k != 0, k);
         }
         top.cut();
     }
@@ -304,7 +346,7 @@ __global__ __launch_bounds__(64 * kWaves) void logprobs_kernel(Logprobs a)
 template <bool BF16>
 __global__ __launch_bounds__(64) void logprobs_join_kernel(Logprobs a)
 {
-    __shared__ key_t lds_keys[kBuffer];
+    __shared__ key_t lds_keys[kSlots];
     const int lane = threadIdx.x;
     const int64_t row = blockIdx.x;
     Sums s = {-kInf, 0.0f, 0.0f};
@@ -316,11 +358,17 @@ __global__ __launch_bounds__(64) void logprobs_join_kernel(Logprobs a)
     Top top = {lds_keys, a.n_top, 0, 0};
     if (a.n_top > 0) {
         const int total = a.segments * a.n_top;
-        for (int i0 = 0; i0 < total; i0 += 64) {
-            const int i = i0 + lane;
-            key_t k = 0;
-            if (i < total) k = segment_keys(a, row, i / a.n_top)[i % a.n_top];
-            top.add(k != 0, k);
+        for (int i0 = 0; i0 < total; i0 += 256) {
+            key_t k[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t i = i0 + 64 * e + lane;
+                k[e] = 0;
+                if (i < (uint32_t)total)
+                    k[e] = segment_keys(a, row, i / (uint32_t)a.n_top)[i % (uint32_t)a.n_top];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top.add_or_cut(k[e] != 0, k[e]);
         }
         top.cut();
     }
