@@ -404,8 +404,19 @@ def group_pmr(W, group_size: int = 128, stream=None):
     return out
 
 
-from .serving import (  # noqa: E402,F401  (uses the names above)
-    CODE_TYPES, RRQ_CODE_FP8, RRQ_CODE_INT8, RRQ_MAX_TOP, CacheBatch, KVCache, RrqBatch, RrqCache,
-    attention_workspace, cache_attention, cache_read, cache_write, logprobs_workspace,
-    rrq_cache_attention, rrq_cache_attention_workspace, rrq_cache_read, rrq_cache_write,
-    rrq_token_logprobs, rrq_token_logprobs_workspace, token_logprobs)
+# serving needs torch at import; its names are loaded with their first use
+_SERVING = frozenset((
+    "CODE_TYPES", "RRQ_CODE_FP8", "RRQ_CODE_INT8", "RRQ_MAX_TOP", "CacheBatch", "KVCache",
+    "RrqBatch", "RrqCache", "attention_workspace", "cache_attention", "cache_read", "cache_write",
+    "logprobs_workspace", "rrq_cache_attention", "rrq_cache_attention_workspace",
+    "rrq_cache_read", "rrq_cache_write", "rrq_token_logprobs", "rrq_token_logprobs_workspace",
+    "token_logprobs"))
+
+
+def __getattr__(name):
+    if name in _SERVING:
+        from . import serving
+        for n in _SERVING:
+            globals()[n] = getattr(serving, n)
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -33,16 +33,20 @@ __device__ __forceinline__ int clamp_length(const Attend &a, int len)
     return len < 0 ? 0 : (len > cap ? (int)cap : len);
 }
 
+// A value that is the same in every lane, told so to the compiler: in a scalar
+// register.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
 // The rows of tile slot u, tiles of R rows.
 template <int R>
 __device__ __forceinline__ bool find_rows(const Attend &a, int u, RowTile &r)
 {
     constexpr int shift = __builtin_ctz(R);
-    const int s = find_sequence(a.batch, u, a.ratio, shift, 1);
+    const int s = uniform(find_sequence(a.batch, u, a.ratio, shift, 1));
     r.seq = s;
-    r.o0 = clamp_row(a.batch, s);
-    const int n = clamp_row(a.batch, s + 1) - r.o0;
-    const int len = a.batch.lengths[s];
+    r.o0 = uniform(clamp_row(a.batch, s));
+    const int n = uniform(clamp_row(a.batch, s + 1)) - r.o0;
+    const int len = uniform(a.batch.lengths[s]);
     r.row0 = (u - ((r.o0 * a.ratio >> shift) + s)) * R;
     r.n_rows = n * a.ratio;
     if (n <= 0 || r.row0 < 0 || r.row0 >= r.n_rows) return false;   // < 0: before the first sequence
@@ -81,8 +85,8 @@ __device__ __forceinline__ void tile_keys(const Attend &a, const RowTile &r, int
                                           int &hi_any, int &lo_all, int &hi_all)
 {
     const int end = r.row0 + R < r.n_rows ? r.row0 + R : r.n_rows;
-    row_keys(a, r, place_of(a, r.row0).token, lo_any, hi_all);
-    row_keys(a, r, place_of(a, end - 1).token, lo_all, hi_any);
+    row_keys(a, r, uniform(place_of(a, r.row0).token), lo_any, hi_all);
+    row_keys(a, r, uniform(place_of(a, end - 1).token), lo_all, hi_any);
 }
 
 // Key tiles of the whole batch, times the row tiles that read them (one kv
@@ -100,7 +104,7 @@ __device__ __forceinline__ int64_t batch_tiles(const Attend &a)
     }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-    return sum;
+    return ((int64_t)uniform((int)(sum >> 32)) << 32) | (uint32_t)uniform((int)sum);
 }
 
 // The key tiles [tb, te) of split number `split` of a row tile that sees
@@ -122,6 +126,7 @@ __device__ __forceinline__ void split_tiles(const Attend &a, int lo, int hi, int
         per = per < want ? want : per;
         per = per < a.min_tiles ? a.min_tiles : per;
     }
+    per = uniform(per);
     tb = split * per < tiles ? t0 + split * per : t0 + tiles;
     te = tb + per < t0 + tiles ? tb + per : t0 + tiles;
 }

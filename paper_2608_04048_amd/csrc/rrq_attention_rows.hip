@@ -72,7 +72,8 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
     constexpr int ND = D / 32, NK = D / 16, NH = KEYS / 32, RUNS = KEYS / 16;
     __shared__ __attribute__((aligned(16))) uint8_t lds[2 * BUF];
 
-    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, hb = lane >> 5;
     const int H = a.cache.n_kv_heads, P = a.cache.page_size;
     // heads are the fastest index: workgroups go to the 8 XCDs in turn, so a
@@ -126,22 +127,37 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
     constexpr int KP = D / 16, KSTEP = 256 / KP, VSTEP = 256 / RUNS;
     const int shift = __builtin_ctz(P);
     const int64_t head_bytes = (int64_t)P * D;
-    const int krow = t / KP, vrun = t % RUNS;
-    u32x4v kw[KT], vw[KT];
-    int page;                           // of the tile after the one in registers
-    float ksr, vsr;                     // of the tile in registers: its scales
+    // With heads of 256 the registers are full (an output of 128, queries of 64
+    // of 256): there keys and values go through the same staging registers in
+    // turn (LEAN), and addresses are formed anew from an opaque thread number
+    // instead of kept.
+    constexpr bool LEAN = D == 256;
+    auto thread = [] {
+        int t = threadIdx.x;
+        if (LEAN) asm volatile("" : "+v"(t));
+        return t;
+    };
+    u32x4v kw[KT], vw_own[LEAN ? 1 : KT];
+    u32x4v(&vw)[KT] = *reinterpret_cast<u32x4v(*)[KT]>(LEAN ? kw : vw_own);
+    int kpage, vpage;                   // pages of the keys and the values to load next
+    float ksr, vsr;                     // scales of the values in registers
     bool absent;                        // and whether the lane's run is absent
     // Loads without a branch: tiles past the last are the last again (staged,
     // never used), a run past the keys has the last key's page, an absent page
     // is read as page 0.
     auto find_page = [&](int tile) {
+        const int vrun = thread() % RUNS;
         const int key = (tile < te ? tile : te - 1) * KEYS + 16 * vrun;
-        page = table[(key < hi_any ? key : hi_any - 1) >> shift];
+        return table[(key < hi_any ? key : hi_any - 1) >> shift];
     };
-    auto load_tile = [&](int tile) {
-        const int key0 = (tile < te ? tile : te - 1) * KEYS, run = key0 + 16 * vrun;
-        absent = run >= hi_any || run + 16 <= lo_any || (uint32_t)page >= (uint64_t)a.cache.n_pages;
-        const int safe = absent ? 0 : page;
+    auto is_absent = [&](int run, int page) {
+        return run >= hi_any || run + 16 <= lo_any ||
+               (uint32_t)page >= (uint64_t)a.cache.n_pages;
+    };
+    auto load_keys = [&](int tile) {
+        const int t = thread(), krow = t / KP;
+        const int key0 = (tile < te ? tile : te - 1) * KEYS;
+        const int safe = is_absent(key0 + 16 * (t % RUNS), kpage) ? 0 : kpage;
 #pragma unroll
         for (int i = 0; i < KT; ++i) {
             const int row0 = KSTEP * i + 64 / KP * wave;        // wave's first row
@@ -150,7 +166,12 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
             kw[i] = *reinterpret_cast<const u32x4v *>(
                 src + (uint32_t)(((key0 + krow + KSTEP * i) & (P - 1)) * D + 16 * (t % KP)));
         }
-        const int64_t block = (int64_t)safe * H + kvh;
+    };
+    auto load_values = [&](int tile) {
+        const int t = thread(), vrun = t % RUNS;
+        const int key0 = (tile < te ? tile : te - 1) * KEYS;
+        absent = is_absent(key0 + 16 * vrun, vpage);
+        const int64_t block = (int64_t)(absent ? 0 : vpage) * H + kvh;
         const uint8_t *src = a.cache.v_codes + block * head_bytes +
                              (uint32_t)((t / RUNS) * P + ((key0 + 16 * vrun) & (P - 1)));
 #pragma unroll
@@ -162,6 +183,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
     // Values of keys that no row sees may be left over from another use of the
     // page (not numbers, even): cleared.
     auto clear_unseen = [&](int tile) {
+        const int vrun = thread() % RUNS;
         const int run = (tile < te ? tile : te - 1) * KEYS + 16 * vrun;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
@@ -175,13 +197,17 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
             for (int i = 0; i < KT; ++i) vw[i][w] &= keep;
         }
     };
-    auto store_tile = [&](uint8_t *buf) {
+    auto store_keys = [&](uint8_t *buf) {
+        const int t = thread(), krow = t / KP;
 #pragma unroll
         for (int i = 0; i < KT; ++i) {
             uint8_t *at = buf + (krow + KSTEP * i) * KROW + 16 * (t % KP);
             *reinterpret_cast<f16x8 *>(at) = codes_f16<CODE>(kw[i][0], kw[i][1]);
             *reinterpret_cast<f16x8 *>(at + D) = codes_f16<CODE>(kw[i][2], kw[i][3]);
         }
+    };
+    auto store_values = [&](uint8_t *buf) {
+        const int t = thread(), vrun = t % RUNS;
 #pragma unroll
         for (int i = 0; i < KT; ++i) {
             uint8_t *at = buf + KB + (t / RUNS + VSTEP * i) * VROW + 32 * vrun;
@@ -213,20 +239,45 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
         for (int e = 0; e < 16; ++e) o[n][e] = 0.0f;
 
     if (tb < te) {
-        find_page(tb);
-        load_tile(tb);
-        find_page(tb + 1);
+        uint8_t *buf = lds + (tb & 1) * BUF;
+        kpage = vpage = find_page(tb);
+        load_keys(tb);
+        if (!LEAN) load_values(tb);
+        kpage = find_page(tb + 1);
+        store_keys(buf);
+        if (LEAN) load_values(tb);
         clear_unseen(tb);
-        store_tile(lds + (tb & 1) * BUF);
-        load_tile(tb + 1);
-        find_page(tb + 2);
+        store_values(buf);
+        load_keys(tb + 1);
+        vpage = kpage;
+        if (!LEAN) load_values(tb + 1);
+        kpage = find_page(tb + 2);
+        if (!LEAN) vpage = kpage;
         barrier();
     }
-    for (int tile = tb; tile < te; ++tile) {
-        const uint8_t *buf = lds + (tile & 1) * BUF;
+    // A wave without rows (the tile's last ones) only stages.
+    const bool busy = r.row0 + 32 * wave < r.n_rows;
+    for (int tile = tb; tile < te && !busy; ++tile) {
+        uint8_t *next = lds + ((tile + 1) & 1) * BUF;
+        store_keys(next);
+        if (LEAN) {
+            load_values(tile + 1);
+            vpage = kpage;
+        }
         if (at_edge(tile + 1) || __any(absent)) clear_unseen(tile + 1);
+        store_values(next);
+        load_keys(tile + 2);
+        if (!LEAN) load_values(tile + 2);
+        kpage = find_page(tile + 3);
+        if (!LEAN) vpage = kpage;
+        barrier();
+    }
+    for (int tile = tb; tile < te && busy; ++tile) {
+        const uint8_t *buf = lds + (tile & 1) * BUF;
+        uint8_t *next = lds + ((tile + 1) & 1) * BUF;
+        if (!LEAN && (at_edge(tile + 1) || __any(absent))) clear_unseen(tile + 1);
         // scales of run lane % RUNS, and the tile's absent runs
-        const f32x2 scales = *reinterpret_cast<const f32x2 *>(buf + KB + VB + 8 * vrun);
+        const f32x2 scales = *reinterpret_cast<const f32x2 *>(buf + KB + VB + 8 * (lane % RUNS));
         const float kst = scales[0], vst = scales[1];
         const uint32_t gone = (uint32_t)__ballot(vst < 0.0f) & ((1u << RUNS) - 1);
 
@@ -235,17 +286,29 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
         for (int h = 0; h < NH; ++h)
 #pragma unroll
             for (int e = 0; e < 16; ++e) s[h][e] = 0.0f;
+        int place = thread();
+        const uint8_t *krows = buf + (place & 31) * KROW + ((place >> 5) & 1) * 16;
 #pragma unroll
-        for (int j = 0; j < NK; ++j)
+        for (int j = 0; j < NK; ++j) {
+            // (operands read ahead by 4 products at most where registers are full)
+            if (D == 256 && j > 0 && j % 4 == 0) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int h = 0; h < NH; ++h) {
-                const f16x8 k = *reinterpret_cast<const f16x8 *>(
-                    buf + (32 * h + col) * KROW + 32 * j + 16 * hb);
+                const f16x8 k =
+                    *reinterpret_cast<const f16x8 *>(krows + 32 * h * KROW + 32 * j);
                 s[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[j], s[h], 0, 0, 0);
             }
-        store_tile(lds + ((tile + 1) & 1) * BUF);
-        load_tile(tile + 2);
-        find_page(tile + 3);
+        }
+        store_keys(next);
+        if (LEAN) {
+            load_values(tile + 1);
+            vpage = kpage;
+        } else {
+            store_values(next);
+            load_keys(tile + 2);
+            load_values(tile + 2);
+            vpage = kpage = find_page(tile + 3);
+        }
 
         if (at_edge(tile) || gone) {
             // -inf stands for a key that the row does not see: its weight is
@@ -308,15 +371,22 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
                 sum = __builtin_amdgcn_fdot2(f16x2{p[i][e], p[i][e + 1]}, ones, sum, false);
             l += sum * back;
         }
+        place = thread();
+        const uint8_t *vrows = buf + KB + (place & 31) * VROW + ((place >> 5) & 1) * 16;
 #pragma unroll
         for (int i = 0; i < RUNS; ++i)
 #pragma unroll
             for (int n = 0; n < ND; ++n) {
-                const f16x8 v = *reinterpret_cast<const f16x8 *>(
-                    buf + KB + (32 * n + col) * VROW + 32 * i + 16 * hb);
+                const f16x8 v =
+                    *reinterpret_cast<const f16x8 *>(vrows + 32 * n * VROW + 32 * i);
                 o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[i], o[n], 0, 0, 0);
             }
-        //SCHED
+        if (LEAN) {
+            if (at_edge(tile + 1) || __any(absent)) clear_unseen(tile + 1);
+            store_values(next);
+            load_keys(tile + 2);
+            kpage = find_page(tile + 3);
+        }
         barrier();
     }
 

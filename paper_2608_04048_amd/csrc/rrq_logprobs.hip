@@ -38,6 +38,11 @@ __device__ __forceinline__ uint32_t ordered(float x)
     if (x != x) return 0;
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
+// The logit of an ordered() value (0: of no number).
+__device__ __forceinline__ float logit_of(uint32_t o)
+{
+    return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
+}
 __device__ __forceinline__ key_t make_key(uint32_t ord, uint32_t index)
 {
     return ((key_t)ord << 32) | (uint32_t)~index;
@@ -132,8 +137,7 @@ struct Top {
     // nothing is below that).
     __device__ float floor_value() const
     {
-        const uint32_t o = (uint32_t)(floor >> 32);
-        return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
+        return logit_of((uint32_t)(floor >> 32));
     }
 
     // Adds the keys of the lanes that have one (every lane calls it); there is
@@ -145,6 +149,17 @@ struct Top {
         const int at = count + __popcll(who & ((1ull << lane) - 1));
         if ((who >> lane) & 1) buf[at] = k;
         count += __popcll(who);
+    }
+    // Raises the floor to just below the largest of the lanes' keys, each the
+    // n-th best of some list (0: of a shorter list).
+    __device__ void raise(key_t nth)
+    {
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const key_t o = __shfl_xor(nth, d);
+            nth = o > nth ? o : nth;
+        }
+        if (nth > floor + 1) floor = nth - 1;
     }
     __device__ void add_or_cut(bool has, key_t k)
     {
@@ -180,30 +195,36 @@ __device__ __forceinline__ key_t *segment_keys(const Logprobs &a, int64_t row, i
     return reinterpret_cast<key_t *>(base);
 }
 
-// The row's results, from its joined sums and its sorted keys (one wave).
+// The row's target logit (lane 0; loaded before it is needed). inside: the
+// target is a token.
 template <bool BF16>
+__device__ __forceinline__ float target_logit(const Logprobs &a, int64_t row, bool &inside)
+{
+    inside = false;
+    if ((threadIdx.x & 63) != 0 || !a.targets) return 0.0f;
+    const int64_t t = a.targets[row];
+    inside = t >= 0 && t < a.vocab;
+    const void *x = static_cast<const char *>(a.logits) + row * a.row_stride * (BF16 ? 2 : 4);
+    return inside ? load_logit<BF16>(x, t) : 0.0f;
+}
+
+// The row's results, from its joined sums and its sorted keys (one wave).
 __device__ __forceinline__ void write_row(const Logprobs &a, int64_t row, const Sums &s,
-                                          const key_t *keys)
+                                          const key_t *keys, float target, bool inside)
 {
     const int lane = threadIdx.x & 63;
-    const void *x = static_cast<const char *>(a.logits) + row * a.row_stride * (BF16 ? 2 : 4);
     // a row of -inf only: l and t are 0 (or NaN, if it holds one)
     const bool empty = s.m == -kInf;
     const float log_l = empty ? s.l : logf(s.l);
     if (lane == 0) {
         if (a.entropy) a.entropy[row] = empty ? s.l : log_l - s.t / s.l;
-        if (a.targets) {
-            const int64_t t = a.targets[row];
-            float r = 0.0f;
-            if (t >= 0 && t < a.vocab)
-                r = (empty ? load_logit<BF16>(x, t) : load_logit<BF16>(x, t) - s.m) - log_l;
-            a.logprobs[row] = r;
-        }
+        if (a.targets)
+            a.logprobs[row] = inside ? (empty ? target : target - s.m) - log_l : 0.0f;
     }
     if (lane < a.n_top) {       // n_top <= vocab: every key is a logit's
-        const uint32_t i = ~(uint32_t)keys[lane];
-        const float v = load_logit<BF16>(x, i);
-        a.top_ids[row * a.n_top + lane] = i;
+        const key_t k = keys[lane];
+        const float v = logit_of((uint32_t)(k >> 32));
+        a.top_ids[row * a.n_top + lane] = (uint32_t)~(uint32_t)k;
         a.top_logprobs[row * a.n_top + lane] = (empty ? v : v - s.m) - log_l;
     }
 }
@@ -308,6 +329,9 @@ __global__ __launch_bounds__(64 * kWaves, 5) void logprobs_kernel(Logprobs a)
         }
         top.cut();
     }
+    bool inside = false;
+    float target = 0.0f;
+    if (a.segments == 1 && wave == 0) target = target_logit<BF16>(a, row, inside);
     s = wave_join(s);
     if (lane == 0) {
         lds_sums[wave][0] = s.m;
@@ -321,6 +345,7 @@ __global__ __launch_bounds__(64 * kWaves, 5) void logprobs_kernel(Logprobs a)
     for (int w = 1; w < kWaves; ++w)
         s = join(s, Sums{lds_sums[w][0], lds_sums[w][1], lds_sums[w][2]});
     if (a.n_top > 0) {
+        top.raise(lane < kWaves ? lds_keys[lane][a.n_top - 1] : 0);
 #pragma unroll 1
         for (int w = 1; w < kWaves; ++w) {
             const key_t k = lane < a.n_top ? lds_keys[w][lane] : 0;
@@ -329,7 +354,7 @@ __global__ __launch_bounds__(64 * kWaves, 5) void logprobs_kernel(Logprobs a)
         top.cut();
     }
     if (a.segments == 1) {
-        write_row<BF16>(a, row, s, top.buf);
+        write_row(a, row, s, top.buf, target, inside);
         return;
     }
     key_t *out = segment_keys(a, row, seg);
@@ -349,30 +374,43 @@ __global__ __launch_bounds__(64) void logprobs_join_kernel(Logprobs a)
     __shared__ key_t lds_keys[kSlots];
     const int lane = threadIdx.x;
     const int64_t row = blockIdx.x;
+    // every load that waits for nothing first
+    bool inside;
+    const float target = target_logit<BF16>(a, row, inside);
+    const uint32_t n = a.n_top, total = a.segments * n;
+    key_t k[4] = {}, nth = 0;
+    auto load_keys = [&](uint32_t i0) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t i = i0 + 64 * e + lane;
+            k[e] = i < total ? segment_keys(a, row, i / n)[i % n] : 0;
+        }
+    };
+    if (n > 0) {
+        load_keys(0);
+        for (int seg = lane; seg < a.segments; seg += 64) {
+            const key_t o = segment_keys(a, row, seg)[n - 1];
+            nth = o > nth ? o : nth;
+        }
+    }
     Sums s = {-kInf, 0.0f, 0.0f};
     for (int seg = lane; seg < a.segments; seg += 64) {
-        const float *sums = reinterpret_cast<const float *>(segment_keys(a, row, seg) + a.n_top);
+        const float *sums = reinterpret_cast<const float *>(segment_keys(a, row, seg) + n);
         s = join(s, Sums{sums[0], sums[1], sums[2]});
     }
     s = wave_join(s);
     Top top = {lds_keys, a.n_top, 0, 0};
-    if (a.n_top > 0) {
-        const int total = a.segments * a.n_top;
-        for (int i0 = 0; i0 < total; i0 += 256) {
-            key_t k[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t i = i0 + 64 * e + lane;
-                k[e] = 0;
-                if (i < (uint32_t)total)
-                    k[e] = segment_keys(a, row, i / (uint32_t)a.n_top)[i % (uint32_t)a.n_top];
-            }
+    if (n > 0) {
+        top.raise(nth);
+        for (uint32_t i0 = 0;;) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) top.add_or_cut(k[e] != 0, k[e]);
+            if ((i0 += 256) >= total) break;
+            load_keys(i0);
         }
         top.cut();
     }
-    write_row<BF16>(a, row, s, lds_keys);
+    write_row(a, row, s, lds_keys, target, inside);
 }
 
 }  // namespace

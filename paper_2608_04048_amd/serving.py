@@ -23,6 +23,8 @@ from __future__ import annotations
 import ctypes
 import math
 
+import torch
+
 from . import (RRQ_BF16, RRQ_F32, RRQ_OK, RRQError, _check_device_tensor, _ptr, _stream,
                load_library)
 
@@ -147,7 +149,6 @@ class KVCache:
     GPU. code_type: "int8" or "fp8" (e4m3)."""
 
     def __init__(self, k_codes, v_codes, k_scales, v_scales, code_type: str = "int8"):
-        import torch
         if code_type not in CODE_TYPES:
             raise ValueError(f"code_type must be one of {sorted(CODE_TYPES)}, got {code_type!r}")
         for t, name, dtype in ((k_codes, "k_codes", torch.uint8), (v_codes, "v_codes", torch.uint8),
@@ -170,14 +171,15 @@ class KVCache:
         self.code_type = code_type
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = pages, heads, page, dim
         self.device = k_codes.device
+        self.index = k_codes.get_device()
         self.desc = RrqCache(_ptr(k_codes), _ptr(v_codes), _ptr(k_scales), _ptr(v_scales), pages,
                              heads, dim, page, CODE_TYPES[code_type])
+        self.ref = ctypes.byref(self.desc)
 
     @classmethod
     def empty(cls, n_pages: int, n_kv_heads: int, head_dim: int, page_size: int = 64,
               code_type: str = "int8", device="cuda") -> "KVCache":
         """A cache of uninitialised pages (a page needs no initial value)."""
-        import torch
         return cls(torch.empty((n_pages, n_kv_heads, page_size, head_dim), dtype=torch.uint8,
                                device=device),
                    torch.empty((n_pages, n_kv_heads, head_dim, page_size), dtype=torch.uint8,
@@ -194,7 +196,6 @@ class CacheBatch:
     call's dense tensors (offsets[n_seqs])."""
 
     def __init__(self, page_table, lengths, offsets, n_tokens: int):
-        import torch
         for t, name in ((page_table, "page_table"), (lengths, "lengths"), (offsets, "offsets")):
             if not isinstance(t, torch.Tensor):
                 raise TypeError(f"{name} must be a torch.Tensor")
@@ -217,53 +218,50 @@ class CacheBatch:
         self.page_table, self.lengths, self.offsets = page_table, lengths, offsets
         self.n_seqs, self.max_pages, self.n_tokens = n_seqs, max_pages, int(n_tokens)
         self.device = page_table.device
+        self.index = page_table.get_device()
+        self.workspace_bytes = {}       # by the cache's sizes and the head count
         self.desc = RrqBatch(_ptr(page_table), _ptr(lengths), _ptr(offsets), stride, max_pages,
                              n_seqs, self.n_tokens)
+        self.ref = ctypes.byref(self.desc)
+
+
+_DTYPES = {torch.float32: RRQ_F32, torch.bfloat16: RRQ_BF16}
 
 
 def _dtype_code(dtype, name: str) -> int:
-    import torch
-    if dtype == torch.float32:
-        return RRQ_F32
-    if dtype == torch.bfloat16:
-        return RRQ_BF16
-    raise TypeError(f"{name} must be torch.float32 or torch.bfloat16, got {dtype}")
+    code = _DTYPES.get(dtype)
+    if code is None:
+        raise TypeError(f"{name} must be torch.float32 or torch.bfloat16, got {dtype}")
+    return code
 
 
-def _check_rows(t, name: str, rows: int, heads, dim: int, device) -> None:
-    """t is [rows, heads, dim] on the device with contiguous last dimension."""
-    import torch
+def _row_strides(t, name: str, rows: int, heads, dim: int, index: int):
+    """Checks that t is [rows, heads, dim] on the GPU of that index with
+    contiguous last dimension. Returns its token and head stride; one that is
+    never used (one token, one head) may be anything, so it counts as 0."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.device != device:
-        raise ValueError(f"{name} must be on {device}, got {t.device}")
+    if t.get_device() != index:
+        raise ValueError(f"{name} must be on cuda:{index}, got {t.device}")
     shape = t.shape
     if len(shape) != 3 or shape[0] != rows or shape[2] != dim or (heads and shape[1] != heads):
         raise ValueError(f"{name} must be [{rows}, {heads or 'heads'}, {dim}], got {tuple(shape)}")
-    if t.stride(2) != 1:
+    token, head, one = t.stride()
+    if one != 1:
         raise ValueError(f"{name} must be contiguous in its last dimension")
+    return token if rows > 1 else 0, head if shape[1] > 1 else 0
 
 
-def _strides(t):
-    """Token and head stride of rows [tokens, heads, dim]; a stride that is
-    never used (one token, one head) may be anything, so it counts as 0."""
-    s = t.stride()
-    return s[0] if t.shape[0] > 1 else 0, s[1] if t.shape[1] > 1 else 0
-
-
-def _check_out(out, name, shape, dtype, device):
+def _check_out(out, name, shape, dtype, index):
     _check_device_tensor(out, name, dtype)
-    if out.device != device or tuple(out.shape) != tuple(shape):
-        raise ValueError(f"{name} must be {tuple(shape)} on {device}, got {tuple(out.shape)} on "
-                         f"{out.device}")
+    if out.get_device() != index or tuple(out.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {tuple(shape)} on cuda:{index}, got {tuple(out.shape)} "
+                         f"on {out.device}")
 
 
 def _used_on(stream, *tensors) -> None:
     """Memory allocated here for the current stream that a kernel on another
     stream uses must not be handed out again before that kernel is done."""
-    import torch
-    if stream is None:
-        return
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream)
     for t in tensors:
@@ -271,71 +269,89 @@ def _used_on(stream, *tensors) -> None:
             t.record_stream(stream)
 
 
-def _same_device(cache, batch) -> None:
-    if cache.device != batch.device:
-        raise ValueError(f"cache and batch must be on one device, got {cache.device} and "
-                         f"{batch.device}")
+def _device_index(cache, batch) -> int:
+    if cache.index != batch.index:
+        raise ValueError(f"cache and batch must be on one device, got cuda:{cache.index} and "
+                         f"cuda:{batch.index}")
+    return cache.index
 
 
 def cache_write(cache: KVCache, batch: CacheBatch, K, V, stream=None) -> None:
     """Quantise keys and values [n_tokens, n_kv_heads, head_dim] (float32 or
     bfloat16, any token and head strides of whole 16 bytes) into the batch's
     pages."""
-    _same_device(cache, batch)
-    for t, name in ((K, "K"), (V, "V")):
-        _check_rows(t, name, batch.n_tokens, cache.n_kv_heads, cache.head_dim, cache.device)
+    index = _device_index(cache, batch)
+    rows, heads, dim = batch.n_tokens, cache.n_kv_heads, cache.head_dim
+    kt, kh = _row_strides(K, "K", rows, heads, dim, index)
+    vt, vh = _row_strides(V, "V", rows, heads, dim, index)
     if K.dtype != V.dtype:
         raise TypeError(f"K and V must have one dtype, got {K.dtype} and {V.dtype}")
-    kt, kh = _strides(K)
-    vt, vh = _strides(V)
-    rrq_cache_write(cache.desc, batch.desc, K, V, _dtype_code(K.dtype, "K"), kt, kh, vt, vh,
-                    stream)
+    st = (_lib or _library()).rrq_cache_write(cache.ref, batch.ref, K.data_ptr(), V.data_ptr(),
+                                              _dtype_code(K.dtype, "K"), kt, kh, vt, vh,
+                                              _stream(stream))
+    if st != RRQ_OK:
+        raise RRQError(st, "rrq_cache_write")
 
 
 def cache_read(cache: KVCache, batch: CacheBatch, dtype=None, stream=None, out=None):
     """(K, V) [n_tokens, n_kv_heads, head_dim] of the batch's tokens, dequantised
     to float32 or bfloat16 (the default). ``out`` may pass the pair."""
-    import torch
-    _same_device(cache, batch)
+    index = _device_index(cache, batch)
     shape = (batch.n_tokens, cache.n_kv_heads, cache.head_dim)
     if out is None:
         dtype = torch.bfloat16 if dtype is None else dtype
         code = _dtype_code(dtype, "dtype")
         K = torch.empty(shape, dtype=dtype, device=cache.device)
-        V = torch.empty(shape, dtype=dtype, device=cache.device)
-        _used_on(stream, K, V)
+        V = torch.empty_like(K)         # (quicker)
+        if stream is not None:
+            _used_on(stream, K, V)
     else:
         K, V = out
-        code = _dtype_code(K.dtype if dtype is None else dtype, "dtype")
-        for t, name in ((K, "out[0]"), (V, "out[1]")):
-            _check_out(t, name, shape, K.dtype if dtype is None else dtype, cache.device)
-    rrq_cache_read(cache.desc, batch.desc, K, V, code, stream)
+        dtype = K.dtype if dtype is None else dtype
+        code = _dtype_code(dtype, "dtype")
+        _check_out(K, "out[0]", shape, dtype, index)
+        _check_out(V, "out[1]", shape, dtype, index)
+    st = (_lib or _library()).rrq_cache_read(cache.ref, batch.ref, K.data_ptr(), V.data_ptr(),
+                                             code, _stream(stream))
+    if st != RRQ_OK:
+        raise RRQError(st, "rrq_cache_read")
     return K, V
 
 
 def _workspace(n_bytes: int, device, stream):
-    import torch
     if n_bytes == 0:
         return None
     w = torch.empty(n_bytes, dtype=torch.uint8, device=device)
-    _used_on(stream, w)
+    if stream is not None:
+        _used_on(stream, w)
     return w
 
 
-def _check_workspace(w, device):
-    import torch
-    if w is not None:
-        _check_device_tensor(w, "workspace", torch.uint8)
-        if w.device != device:
-            raise ValueError(f"workspace must be on {device}, got {w.device}")
+def _workspace_args(w, index: int):
+    """Address and bytes of a caller's workspace."""
+    if w is None:
+        return None, 0
+    if (not isinstance(w, torch.Tensor) or w.dtype != torch.uint8 or w.get_device() != index or
+            not w.is_contiguous()):
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on cuda:{index}")
+    return w.data_ptr(), w.numel()
+
+
+def _attention_bytes(cache, batch, n_heads: int) -> int:
+    # (a function of these sizes alone)
+    key = (cache.n_kv_heads, cache.head_dim, cache.page_size, n_heads)
+    n = batch.workspace_bytes.get(key)
+    if n is None:
+        n = rrq_cache_attention_workspace(cache.desc, batch.desc, n_heads)
+        batch.workspace_bytes[key] = n
+    return n
 
 
 def attention_workspace(cache: KVCache, batch: CacheBatch, n_heads: int):
     """A workspace for cache_attention on this cache, batch and head count
     (uint8 tensor, or None if none is needed). Calls that may run at the same
     time need their own."""
-    return _workspace(rrq_cache_attention_workspace(cache.desc, batch.desc, n_heads),
-                      cache.device, None)
+    return _workspace(_attention_bytes(cache, batch, n_heads), cache.device, None)
 
 
 def cache_attention(cache: KVCache, batch: CacheBatch, Q, scale=None, causal: bool = True,
@@ -343,28 +359,30 @@ def cache_attention(cache: KVCache, batch: CacheBatch, Q, scale=None, causal: bo
     """Attention of queries [n_tokens, n_heads, head_dim] (float32 or bfloat16)
     over the batch's sequences: [n_tokens, n_heads, head_dim] in bfloat16 (the
     default) or float32. scale defaults to head_dim ** -0.5; window 0 is none."""
-    import torch
-    _same_device(cache, batch)
-    _check_rows(Q, "Q", batch.n_tokens, None, cache.head_dim, cache.device)
-    n_heads = Q.shape[1]
-    if scale is None:
-        scale = 1.0 / math.sqrt(cache.head_dim)
+    index = _device_index(cache, batch)
+    dim = cache.head_dim
+    qt, qh = _row_strides(Q, "Q", batch.n_tokens, None, dim, index)
+    shape = Q.shape
+    n_heads = shape[1]
     if out is None:
-        out = torch.empty((batch.n_tokens, n_heads, cache.head_dim), device=cache.device,
-                          dtype=torch.bfloat16 if out_dtype is None else out_dtype)
-        _used_on(stream, out)
+        out_dtype = torch.bfloat16 if out_dtype is None else out_dtype
+        out_code = _dtype_code(out_dtype, "out_dtype")
+        out = torch.empty(shape, dtype=out_dtype, device=cache.device)
+        if stream is not None:
+            _used_on(stream, out)
     else:
-        _check_out(out, "out", Q.shape, out.dtype if out_dtype is None else out_dtype,
-                   cache.device)
+        out_dtype = out.dtype if out_dtype is None else out_dtype
+        out_code = _dtype_code(out_dtype, "out")
+        _check_out(out, "out", shape, out_dtype, index)
     if workspace is None:
-        workspace = _workspace(rrq_cache_attention_workspace(cache.desc, batch.desc, n_heads),
-                               cache.device, stream)
-    else:
-        _check_workspace(workspace, cache.device)
-    qt, qh = _strides(Q)
-    rrq_cache_attention(cache.desc, batch.desc, Q, _dtype_code(Q.dtype, "Q"), qt, qh, n_heads,
-                        scale, 1 if causal else 0, window, out, _dtype_code(out.dtype, "out"),
-                        workspace, 0 if workspace is None else workspace.numel(), stream)
+        workspace = _workspace(_attention_bytes(cache, batch, n_heads), cache.device, stream)
+    w, w_bytes = _workspace_args(workspace, index)
+    st = (_lib or _library()).rrq_cache_attention(
+        cache.ref, batch.ref, Q.data_ptr(), _dtype_code(Q.dtype, "Q"), qt, qh, n_heads,
+        1.0 / math.sqrt(dim) if scale is None else scale, 1 if causal else 0, window,
+        out.data_ptr(), out_code, w, w_bytes, _stream(stream))
+    if st != RRQ_OK:
+        raise RRQError(st, "rrq_cache_attention")
     return out
 
 
@@ -381,35 +399,41 @@ def token_logprobs(logits, targets=None, n_top: int = 0, workspace=None, stream=
     row's target (int64 [rows]; one outside the vocabulary gives 0), the
     entropy, and the n_top likeliest tokens. logprobs is None without targets,
     top_ids and top_logprobs are None for n_top = 0."""
-    import torch
     if not isinstance(logits, torch.Tensor):
         raise TypeError("logits must be a torch.Tensor")
-    if not logits.is_cuda:
+    index = logits.get_device()
+    if index < 0:
         raise ValueError(f"logits must be on a GPU device, got {logits.device}")
     code = _dtype_code(logits.dtype, "logits")
     if logits.dim() != 2:
         raise ValueError(f"logits must be [rows, vocab], got {tuple(logits.shape)}")
     rows, vocab = logits.shape
-    if vocab > 1 and logits.stride(1) != 1:
+    row_stride, one = logits.stride()
+    if vocab > 1 and one != 1:
         raise ValueError("logits must be contiguous in its last dimension")
     device = logits.device
-    logprobs = top_ids = top_logprobs = None
+    logprobs = top_ids = top_logprobs = target_ptr = logprob_ptr = id_ptr = top_ptr = None
     if targets is not None:
-        _check_device_tensor(targets, "targets", torch.int64)
-        if tuple(targets.shape) != (rows,) or targets.device != device:
-            raise ValueError(f"targets must be [{rows}] on {device}, got {tuple(targets.shape)} "
-                             f"on {targets.device}")
+        if (not isinstance(targets, torch.Tensor) or targets.dtype != torch.int64 or
+                targets.get_device() != index or tuple(targets.shape) != (rows,) or
+                not targets.is_contiguous()):
+            raise ValueError(f"targets must be a contiguous int64 tensor [{rows}] on {device}")
         logprobs = torch.empty(rows, dtype=torch.float32, device=device)
-    entropy = torch.empty(rows, dtype=torch.float32, device=device)
+        target_ptr, logprob_ptr = targets.data_ptr(), logprobs.data_ptr()
+    entropy = (torch.empty(rows, dtype=torch.float32, device=device) if logprobs is None else
+               torch.empty_like(logprobs))
     if n_top:
         top_ids = torch.empty((rows, n_top), dtype=torch.int64, device=device)
         top_logprobs = torch.empty((rows, n_top), dtype=torch.float32, device=device)
-    _used_on(stream, logprobs, entropy, top_ids, top_logprobs)
+        id_ptr, top_ptr = top_ids.data_ptr(), top_logprobs.data_ptr()
+    if stream is not None:
+        _used_on(stream, logprobs, entropy, top_ids, top_logprobs)
     if workspace is None:
         workspace = _workspace(rrq_token_logprobs_workspace(rows, vocab, n_top), device, stream)
-    else:
-        _check_workspace(workspace, device)
-    rrq_token_logprobs(logits, code, rows, vocab, logits.stride(0) if rows > 1 else vocab,
-                       targets, n_top, logprobs, entropy, top_ids, top_logprobs, workspace,
-                       0 if workspace is None else workspace.numel(), stream)
+    w, w_bytes = _workspace_args(workspace, index)
+    st = (_lib or _library()).rrq_token_logprobs(
+        logits.data_ptr(), code, rows, vocab, row_stride if rows > 1 else vocab, target_ptr, n_top,
+        logprob_ptr, entropy.data_ptr(), id_ptr, top_ptr, w, w_bytes, _stream(stream))
+    if st != RRQ_OK:
+        raise RRQError(st, "rrq_token_logprobs")
     return logprobs, entropy, top_ids, top_logprobs
