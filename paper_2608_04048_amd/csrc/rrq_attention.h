@@ -90,45 +90,54 @@ __device__ __forceinline__ void tile_keys(const Attend &a, const RowTile &r, int
 }
 
 // Key tiles of the whole batch, times the row tiles that read them (one kv
-// head): what the splits share out. Every lane calls it.
+// head), about: what the splits share out. Every lane calls it.
 template <int R>
-__device__ __forceinline__ int64_t batch_tiles(const Attend &a)
+__device__ __forceinline__ float batch_tiles(const Attend &a)
 {
-    int64_t sum = 0;
+    const int span = R / a.ratio + 1;           // tokens of a row tile
+    float sum = 0.0f;
     for (int s = threadIdx.x & 63; s < a.batch.n_seqs; s += 64) {
         const int n = clamp_row(a.batch, s + 1) - clamp_row(a.batch, s);
         if (n <= 0) continue;
         int64_t keys = clamp_length(a, a.batch.lengths[s]);
-        if (a.window > 0 && keys > a.window + n) keys = a.window + n;
-        sum += ((keys + kTileKeys - 1) >> 6) * ((n * a.ratio + R - 1) / R);
+        if (a.causal) keys -= n / 2 < keys ? n / 2 : keys;
+        if (a.window > 0 && keys > a.window + span) keys = a.window + span;
+        sum += (float)((keys + kTileKeys - 1) / kTileKeys) * (float)((n * a.ratio + R - 1) / R);
     }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-    return ((int64_t)uniform((int)(sum >> 32)) << 32) | (uint32_t)uniform((int)sum);
+    return sum;
 }
 
 // The key tiles [tb, te) of split number `split` of a row tile that sees
-// [lo, hi). Splits are of one size over the whole batch as far as their
-// number allows, so that long sequences take more of them.
+// [lo, hi). Splits are of about one size over the whole batch as far as their
+// number allows, so that long sequences take more of them; a range of up to
+// 1.5 times that size stays whole (two halves would cost more in written and
+// joined outputs than they save). Returns whether split 0 has the whole range:
+// it then writes the result itself and leaves kAlone where the join looks for
+// its sum.
+constexpr float kAlone = -1.0f;
 template <int R>
-__device__ __forceinline__ void split_tiles(const Attend &a, int lo, int hi, int split, int &tb,
+__device__ __forceinline__ bool split_tiles(const Attend &a, int lo, int hi, int split, int &tb,
                                             int &te)
 {
     const int t0 = lo / kTileKeys;
     const int tiles = hi > lo ? (hi + kTileKeys - 1) / kTileKeys - t0 : 0;
-    int per = tiles;
+    int per = tiles, n = 1;
     if (a.n_splits > 1) {
-        // (the mean to a rounding of binary32 will do)
-        const float even = (float)batch_tiles<R>(a) * (float)a.cache.n_kv_heads / (float)a.target;
-        per = (int)((uint32_t)(tiles + a.n_splits - 1) / (uint32_t)a.n_splits);
-        const int most = 1 << 26;
-        const int want = even < (float)most ? (int)even + 1 : most;
-        per = per < want ? want : per;
-        per = per < a.min_tiles ? a.min_tiles : per;
+        float share = batch_tiles<R>(a) * (float)a.cache.n_kv_heads / (float)a.target;
+        share = fmaxf(share, (float)a.min_tiles);
+        if ((float)tiles > 1.5f * share) {
+            const float want = ceilf((float)tiles / share);
+            n = want < (float)a.n_splits ? (int)want : a.n_splits;
+            per = (int)((uint32_t)(tiles + n - 1) / (uint32_t)n);
+        }
     }
+    n = uniform(n);
     per = uniform(per);
     tb = split * per < tiles ? t0 + split * per : t0 + tiles;
     te = tb + per < t0 + tiles ? tb + per : t0 + tiles;
+    return n == 1;
 }
 
 // N query values of the element offset `at` on.

@@ -73,7 +73,8 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
     int lo, hi, lo_any, hi_any, lo_all, hi_all, tb, te;
     row_keys(a, r, place.token, lo, hi);
     tile_keys<kFewTile>(a, r, lo_any, hi_any, lo_all, hi_all);
-    split_tiles<kFewTile>(a, lo_any, hi_any, split, tb, te);
+    const bool alone = split_tiles<kFewTile>(a, lo_any, hi_any, split, tb, te);
+    if (alone && split > 0) return;
 
     const int P = a.cache.page_size, H = a.cache.n_kv_heads;
     const int shift = __builtin_ctz(P);
@@ -248,7 +249,8 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
         const RowPlace place = place_of(a, r.row0 + orow);
         const int64_t at = (int64_t)(r.o0 + place.token) * a.n_heads + kvh * a.ratio +
                            place.member;
-        if (a.n_splits > 1) {
+        if (alone && a.n_splits > 1 && d == 0) a.part_ml[2 * at + 1] = kAlone;
+        if (!alone) {
             const int64_t part = (int64_t)split * a.batch.n_tokens * a.n_heads + at;
             if (d == 0) {
                 a.part_ml[2 * part] = mm;
@@ -266,22 +268,26 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
     }
 }
 
-// Joins the key ranges of a row (token, head): one workgroup of W waves a row,
-// wave w takes ranges w, w + W, ... Lane s holds range s's maximum and sum, so
-// the factors cost one load. The ranges up to the last with a sum were all
-// written; they are read four at a time, those past it as the last, times 0.
+// Joins the key ranges of a row (token, head): W waves a row, wave w takes
+// ranges w, w + W, ..., 4 / W rows a workgroup. Lane s holds range s's maximum
+// and sum, so the factors cost one load. The ranges up to the last with a sum
+// were all written; they are read four at a time, those past it as the last,
+// times 0.
 template <int D, int W>
-__global__ __launch_bounds__(64 * W) void attend_join_kernel(Attend a)
+__global__ __launch_bounds__(256) void attend_join_kernel(Attend a)
 {
     constexpr int N = D / 64;
-    __shared__ float lds[W][D];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t rows = a.batch.n_tokens * a.n_heads, at = blockIdx.x;
+    __shared__ float lds[W > 1 ? W : 1][W > 1 ? D : 1];
+    const int lane = threadIdx.x & 63, wave = (threadIdx.x >> 6) % W;
+    const int64_t rows = a.batch.n_tokens * a.n_heads;
+    const int64_t at = (int64_t)blockIdx.x * (4 / W) + (threadIdx.x >> 6) / W;
+    if (at >= rows) return;
     f32x2 ml = {-kInf, 0.0f};
     if (lane < a.n_splits)
         ml = *reinterpret_cast<const f32x2 *>(a.part_ml + 2 * (lane * rows + at));
-    const int token = (int)(blockIdx.x / (uint32_t)a.n_heads);
+    const int token = (int)((uint32_t)at / (uint32_t)a.n_heads);
     if (token < clamp_row(a.batch, 0) || token >= clamp_row(a.batch, (int)a.batch.n_seqs)) return;
+    if (__shfl(ml[1], 0) == kAlone) return;     // written already
     float m = ml[0];
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
@@ -308,7 +314,7 @@ __global__ __launch_bounds__(64 * W) void attend_join_kernel(Attend a)
             for (int d = 0; d < N; ++d) y[d] += fs * x[i][d];
         }
     }
-    if (W > 1) {
+    if constexpr (W > 1) {
 #pragma unroll
         for (int d = 0; d < N; ++d) lds[wave][lane * N + d] = y[d];
         __syncthreads();
@@ -357,7 +363,7 @@ hipError_t join_dim(const Attend &a, hipStream_t stream)
     if (a.n_splits > 8)
         attend_join_kernel<D, 4><<<rows, 256, 0, stream>>>(a);
     else
-        attend_join_kernel<D, 1><<<rows, 64, 0, stream>>>(a);
+        attend_join_kernel<D, 1><<<(rows + 3) / 4, 256, 0, stream>>>(a);
     return hipGetLastError();
 }
 
@@ -379,9 +385,9 @@ AttendPlan attend_plan(const rrq_cache &c, const rrq_batch &b, int n_heads)
         p.waves = many_waves(c.head_dim);
         return p;
     }
-    p.target = p.rows_form ? 512 : 2048;
-    p.min_tiles = 8;
-    if (units >= (p.rows_form ? kServeCus : p.target)) return p;
+    p.target = p.rows_form ? 768 : 2048;
+    p.min_tiles = p.rows_form && c.head_dim > 64 ? 16 : 8;
+    if (units >= (p.rows_form ? 4 * kServeCus : p.target)) return p;
     const int64_t most = (cap + p.min_tiles * kTileKeys - 1) / (p.min_tiles * kTileKeys);
     int64_t n = 4 * p.target / units;
     n = n > most ? most : n;

@@ -92,7 +92,8 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
     row_keys(a, r, place.token, lo, hi);
     tile_keys<R>(a, r, lo_any, hi_any, lo_all, hi_all);
     int tb, te;
-    split_tiles<R>(a, lo_any, hi_any, blockIdx.y, tb, te);
+    const bool alone = split_tiles<R>(a, lo_any, hi_any, blockIdx.y, tb, te);
+    if (alone && blockIdx.y > 0) return;
     tb *= kTileKeys / KEYS;                 // to tiles of KEYS
     te *= kTileKeys / KEYS;
     const int32_t *table = a.batch.page_table + r.seq * a.batch.table_stride;
@@ -128,19 +129,16 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
     const int shift = __builtin_ctz(P);
     const int64_t head_bytes = (int64_t)P * D;
     // With heads of 256 the registers are full (an output of 128, queries of 64
-    // of 256): there keys and values go through the same staging registers in
-    // turn (LEAN), and addresses are formed anew from an opaque thread number
+    // of 256): there addresses are formed anew from an opaque thread number
     // instead of kept.
-    constexpr bool LEAN = D == 256;
     auto thread = [] {
         int t = threadIdx.x;
-        if (LEAN) asm volatile("" : "+v"(t));
+        if (D == 256) asm volatile("" : "+v"(t));
         return t;
     };
-    u32x4v kw[KT], vw_own[LEAN ? 1 : KT];
-    u32x4v(&vw)[KT] = *reinterpret_cast<u32x4v(*)[KT]>(LEAN ? kw : vw_own);
-    int kpage, vpage;                   // pages of the keys and the values to load next
-    float ksr, vsr;                     // scales of the values in registers
+    u32x4v kw[KT], vw[KT];
+    int page;                           // of the tile after the one in registers
+    float ksr, vsr;                     // of the tile in registers: its scales
     bool absent;                        // and whether the lane's run is absent
     // Loads without a branch: tiles past the last are the last again (staged,
     // never used), a run past the keys has the last key's page, an absent page
@@ -148,16 +146,14 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
     auto find_page = [&](int tile) {
         const int vrun = thread() % RUNS;
         const int key = (tile < te ? tile : te - 1) * KEYS + 16 * vrun;
-        return table[(key < hi_any ? key : hi_any - 1) >> shift];
+        page = table[(key < hi_any ? key : hi_any - 1) >> shift];
     };
-    auto is_absent = [&](int run, int page) {
-        return run >= hi_any || run + 16 <= lo_any ||
-               (uint32_t)page >= (uint64_t)a.cache.n_pages;
-    };
-    auto load_keys = [&](int tile) {
-        const int t = thread(), krow = t / KP;
-        const int key0 = (tile < te ? tile : te - 1) * KEYS;
-        const int safe = is_absent(key0 + 16 * (t % RUNS), kpage) ? 0 : kpage;
+    auto load_tile = [&](int tile) {
+        const int t = thread(), krow = t / KP, vrun = t % RUNS;
+        const int key0 = (tile < te ? tile : te - 1) * KEYS, run = key0 + 16 * vrun;
+        absent = run >= hi_any || run + 16 <= lo_any ||
+                 (uint32_t)page >= (uint64_t)a.cache.n_pages;
+        const int safe = absent ? 0 : page;
 #pragma unroll
         for (int i = 0; i < KT; ++i) {
             const int row0 = KSTEP * i + 64 / KP * wave;        // wave's first row
@@ -166,12 +162,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
             kw[i] = *reinterpret_cast<const u32x4v *>(
                 src + (uint32_t)(((key0 + krow + KSTEP * i) & (P - 1)) * D + 16 * (t % KP)));
         }
-    };
-    auto load_values = [&](int tile) {
-        const int t = thread(), vrun = t % RUNS;
-        const int key0 = (tile < te ? tile : te - 1) * KEYS;
-        absent = is_absent(key0 + 16 * vrun, vpage);
-        const int64_t block = (int64_t)(absent ? 0 : vpage) * H + kvh;
+        const int64_t block = (int64_t)safe * H + kvh;
         const uint8_t *src = a.cache.v_codes + block * head_bytes +
                              (uint32_t)((t / RUNS) * P + ((key0 + 16 * vrun) & (P - 1)));
 #pragma unroll
@@ -197,17 +188,14 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
             for (int i = 0; i < KT; ++i) vw[i][w] &= keep;
         }
     };
-    auto store_keys = [&](uint8_t *buf) {
-        const int t = thread(), krow = t / KP;
+    auto store_tile = [&](uint8_t *buf) {
+        const int t = thread(), krow = t / KP, vrun = t % RUNS;
 #pragma unroll
         for (int i = 0; i < KT; ++i) {
             uint8_t *at = buf + (krow + KSTEP * i) * KROW + 16 * (t % KP);
             *reinterpret_cast<f16x8 *>(at) = codes_f16<CODE>(kw[i][0], kw[i][1]);
             *reinterpret_cast<f16x8 *>(at + D) = codes_f16<CODE>(kw[i][2], kw[i][3]);
         }
-    };
-    auto store_values = [&](uint8_t *buf) {
-        const int t = thread(), vrun = t % RUNS;
 #pragma unroll
         for (int i = 0; i < KT; ++i) {
             uint8_t *at = buf + KB + (t / RUNS + VSTEP * i) * VROW + 32 * vrun;
@@ -239,43 +227,27 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
         for (int e = 0; e < 16; ++e) o[n][e] = 0.0f;
 
     if (tb < te) {
-        uint8_t *buf = lds + (tb & 1) * BUF;
-        kpage = vpage = find_page(tb);
-        load_keys(tb);
-        if (!LEAN) load_values(tb);
-        kpage = find_page(tb + 1);
-        store_keys(buf);
-        if (LEAN) load_values(tb);
+        find_page(tb);
+        load_tile(tb);
+        find_page(tb + 1);
         clear_unseen(tb);
-        store_values(buf);
-        load_keys(tb + 1);
-        vpage = kpage;
-        if (!LEAN) load_values(tb + 1);
-        kpage = find_page(tb + 2);
-        if (!LEAN) vpage = kpage;
+        store_tile(lds + (tb & 1) * BUF);
+        load_tile(tb + 1);
+        find_page(tb + 2);
         barrier();
     }
     // A wave without rows (the tile's last ones) only stages.
     const bool busy = r.row0 + 32 * wave < r.n_rows;
     for (int tile = tb; tile < te && !busy; ++tile) {
-        uint8_t *next = lds + ((tile + 1) & 1) * BUF;
-        store_keys(next);
-        if (LEAN) {
-            load_values(tile + 1);
-            vpage = kpage;
-        }
         if (at_edge(tile + 1) || __any(absent)) clear_unseen(tile + 1);
-        store_values(next);
-        load_keys(tile + 2);
-        if (!LEAN) load_values(tile + 2);
-        kpage = find_page(tile + 3);
-        if (!LEAN) vpage = kpage;
+        store_tile(lds + ((tile + 1) & 1) * BUF);
+        load_tile(tile + 2);
+        find_page(tile + 3);
         barrier();
     }
     for (int tile = tb; tile < te && busy; ++tile) {
         const uint8_t *buf = lds + (tile & 1) * BUF;
-        uint8_t *next = lds + ((tile + 1) & 1) * BUF;
-        if (!LEAN && (at_edge(tile + 1) || __any(absent))) clear_unseen(tile + 1);
+        if (at_edge(tile + 1) || __any(absent)) clear_unseen(tile + 1);
         // scales of run lane % RUNS, and the tile's absent runs
         const f32x2 scales = *reinterpret_cast<const f32x2 *>(buf + KB + VB + 8 * (lane % RUNS));
         const float kst = scales[0], vst = scales[1];
@@ -299,16 +271,9 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
                 s[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[j], s[h], 0, 0, 0);
             }
         }
-        store_keys(next);
-        if (LEAN) {
-            load_values(tile + 1);
-            vpage = kpage;
-        } else {
-            store_values(next);
-            load_keys(tile + 2);
-            load_values(tile + 2);
-            vpage = kpage = find_page(tile + 3);
-        }
+        store_tile(lds + ((tile + 1) & 1) * BUF);
+        load_tile(tile + 2);
+        find_page(tile + 3);
 
         if (at_edge(tile) || gone) {
             // -inf stands for a key that the row does not see: its weight is
@@ -381,12 +346,6 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
                     *reinterpret_cast<const f16x8 *>(vrows + 32 * n * VROW + 32 * i);
                 o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[i], o[n], 0, 0, 0);
             }
-        if (LEAN) {
-            if (at_edge(tile + 1) || __any(absent)) clear_unseen(tile + 1);
-            store_values(next);
-            load_keys(tile + 2);
-            kpage = find_page(tile + 3);
-        }
         barrier();
     }
 
@@ -394,7 +353,8 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
     l += __shfl_xor(l, 32);
     if (!live) return;
     const int64_t at = (r.o0 + token) * a.n_heads + head;
-    if (a.n_splits > 1) {
+    if (alone && a.n_splits > 1 && hb == 0) a.part_ml[2 * at + 1] = kAlone;
+    if (!alone) {
         const int64_t part = (int64_t)blockIdx.y * a.batch.n_tokens * a.n_heads + at;
         if (hb == 0) {
             a.part_ml[2 * part] = m;
