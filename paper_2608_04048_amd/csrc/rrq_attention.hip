@@ -2,8 +2,8 @@
 // for few query rows a sequence (single tokens, drafted tokens), the join of
 // split key ranges, and the choice of form.
 //
-// One workgroup takes a tile of 16 rows (token, query head of the kv head's
-// group) and a range of key positions; its waves take 64-key tiles of the
+// One workgroup takes a tile of 16 or 32 rows (token, query head of the kv
+// head's group) and a range of key positions; its waves take 64-key tiles of the
 // range in turn, each with its own running maximum, sum and output, and are
 // joined at the end. The cache's bytes bound it: codes go from memory to
 // registers, each read once. A row tile whose range is split over several
@@ -27,11 +27,16 @@ namespace {
 // then reaches 2^-28 below the largest weight.
 constexpr float kWeightScale = 0x1p14f;
 
-// Maximum over the four lane groups.
+// Maximum over the four lane groups: the swaps exchange the second halves of
+// rows (of the wave) of one copy with the first of the other.
 __device__ __forceinline__ float group_max(float a)
 {
-    a = fmaxf(a, __shfl_xor(a, 16));
-    return fmaxf(a, __shfl_xor(a, 32));
+    const uint32_t x = __float_as_uint(a);
+    const auto u = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    a = fmaxf(__uint_as_float(u[0]), __uint_as_float(u[1]));
+    const uint32_t y = __float_as_uint(a);
+    const auto v = __builtin_amdgcn_permlane32_swap(y, y, false, false);
+    return fmaxf(__uint_as_float(v[0]), __uint_as_float(v[1]));
 }
 __device__ __forceinline__ float group_sum(float a)
 {
@@ -51,63 +56,30 @@ constexpr unsigned few_lds(int D, int waves, int rows)
 // registers of a compute unit hold.
 constexpr int many_waves(int D) { return D == 64 ? 16 : 8; }
 
-template <int D, int CODE, int NW>
+// NW: waves; NQ: blocks of 16 rows of the row tile.
+template <int D, int CODE, int NW, int NQ>
 __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_kernel(Attend a)
 {
     constexpr int KL = D / 64;      // 16-byte key loads a lane and key row
     constexpr int ND = D / 16;      // 16-channel tiles of the output
+    constexpr int R = 16 * NQ;
     extern __shared__ __attribute__((aligned(16))) float lds[];
     const int rows_max = a.lds_rows;
     float *lds_ml = lds + NW * rows_max * (D + 4);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, g = lane >> 4;
     const int kvh = blockIdx.y, split = blockIdx.z;
     RowTile r;
-    if (!find_rows<kFewTile>(a, blockIdx.x, r)) return;
-
-    // this lane's row
-    const int row = r.row0 + col;
-    const RowPlace place = place_of(a, row < r.n_rows ? row : r.n_rows - 1);
-    const int64_t token = place.token;
-    const int head = kvh * a.ratio + place.member;
-    int lo, hi, lo_any, hi_any, lo_all, hi_all, tb, te;
-    row_keys(a, r, place.token, lo, hi);
-    tile_keys<kFewTile>(a, r, lo_any, hi_any, lo_all, hi_all);
-    const bool alone = split_tiles<kFewTile>(a, lo_any, hi_any, split, tb, te);
+    if (!find_rows<R>(a, blockIdx.x, r)) return;
+    int lo_any, hi_any, lo_all, hi_all, tb, te;
+    tile_keys<R>(a, r, lo_any, hi_any, lo_all, hi_all);
+    const bool alone = split_tiles<R>(a, lo_any, hi_any, split, tb, te);
     if (alone && split > 0) return;
 
     const int P = a.cache.page_size, H = a.cache.n_kv_heads;
     const int shift = __builtin_ctz(P);
     const int32_t *table = a.batch.page_table + r.seq * a.batch.table_stride;
-
-    // Queries: lane (col, g) holds channels 64 j + 16 g .. + 15 of its row.
-    f16x8 q[KL][2];
-    float qf;
-    {
-        float x[KL][16];
-        float amax = 0.0f;
-        const int64_t at = (r.o0 + token) * a.q_token + head * a.q_head + 16 * g;
-#pragma unroll
-        for (int j = 0; j < KL; ++j) {
-            load_query<16>(a, at + 64 * j, x[j]);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) amax = fmaxf(amax, fabsf(x[j][e]));
-        }
-        float up;
-        query_factors(a, group_max(amax), up, qf);
-#pragma unroll
-        for (int j = 0; j < KL; ++j)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) q[j][h][i] = (_Float16)(x[j][8 * h + i] * up);
-    }
-
-    float m = -kInf, l = 0.0f, vref = 0.0f;
-    f32x4 o[ND];
-#pragma unroll
-    for (int n = 0; n < ND; ++n) o[n] = f32x4{0, 0, 0, 0};
-
     // page number of the run of 16 keys at `key`, -1 if no row sees one of them
     auto page_of = [&](int key) {
         return key < hi_any && key + 16 > lo_any ? table[key >> shift] : -1;
@@ -119,6 +91,47 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
         kpage = page_of((tb + wave) * kTileKeys + 16 * (col >> 2));
         opage = page_of((tb + wave) * kTileKeys + 16 * g);
     }
+
+    // This lane's rows, and their queries: lane (col, g) holds channels
+    // 64 j + 16 g .. + 15.
+    int lo[NQ], hi[NQ];
+    f16x8 q[NQ][KL][2];
+    float qf[NQ];
+#pragma unroll
+    for (int b = 0; b < NQ; ++b) {
+        const int row = r.row0 + 16 * b + col;
+        const RowPlace place = place_of(a, row < r.n_rows ? row : r.n_rows - 1);
+        row_keys(a, r, place.token, lo[b], hi[b]);
+        float x[KL][16];
+        float amax = 0.0f;
+        const int64_t at = (int64_t)(r.o0 + place.token) * a.q_token +
+                           (kvh * a.ratio + place.member) * a.q_head + 16 * g;
+#pragma unroll
+        for (int j = 0; j < KL; ++j) {
+            load_query<16>(a, at + 64 * j, x[j]);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) amax = fmaxf(amax, fabsf(x[j][e]));
+        }
+        float up;
+        query_factors(a, group_max(amax), up, qf[b]);
+#pragma unroll
+        for (int j = 0; j < KL; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) q[b][j][h][i] = (_Float16)(x[j][8 * h + i] * up);
+    }
+
+    float m[NQ], l[NQ], vref = 0.0f;
+    f32x4 o[NQ][ND];
+#pragma unroll
+    for (int b = 0; b < NQ; ++b) {
+        m[b] = -kInf;
+        l[b] = 0.0f;
+#pragma unroll
+        for (int n = 0; n < ND; ++n) o[b][n] = f32x4{0, 0, 0, 0};
+    }
+
     for (int tile = tb + wave; tile < te; tile += NW) {
         const int key0 = tile * kTileKeys;
         const int krun = key0 + 16 * (col >> 2), orun = key0 + 16 * g;
@@ -145,31 +158,40 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
         }
 
         // a lane's 16 keys: orun + 4 i + c
-        float s[4][4];
+        float s[NQ][4][4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            f32x4 acc = {0, 0, 0, 0};
+            f32x4 acc[NQ];
 #pragma unroll
-            for (int j = 0; j < KL; ++j) {
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-                    codes_f16<CODE>(kw[i][j][0], kw[i][j][1]), q[j][0], acc, 0, 0, 0);
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-                    codes_f16<CODE>(kw[i][j][2], kw[i][j][3]), q[j][1], acc, 0, 0, 0);
-            }
+            for (int b = 0; b < NQ; ++b) acc[b] = f32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int c = 0; c < 4; ++c) s[i][c] = acc[c] * (ks * qf);
+            for (int j = 0; j < KL; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const f16x8 k = codes_f16<CODE>(kw[i][j][2 * h], kw[i][j][2 * h + 1]);
+#pragma unroll
+                    for (int b = 0; b < NQ; ++b)
+                        acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[b][j][h], acc[b], 0,
+                                                                        0, 0);
+                }
+#pragma unroll
+            for (int b = 0; b < NQ; ++b)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) s[b][i][c] = acc[b][c] * (ks * qf[b]);
         }
         // Keys a row does not see. The codes there may be left over from
         // another use of the page (not numbers, even), so scores are replaced
         // and value codes of keys that no row sees are cleared.
         if (key0 < lo_all || key0 + kTileKeys > hi_all || !__all(there)) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int b = 0; b < NQ; ++b)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const int key = orun + 4 * i + c;
-                    if (key < lo || key >= hi || !there) s[i][c] = -kInf;
-                }
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int key = orun + 4 * i + c;
+                        if (key < lo[b] || key >= hi[b] || !there) s[b][i][c] = -kInf;
+                    }
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
                 uint32_t keep = 0;
@@ -182,89 +204,102 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
                 for (int n = 0; n < ND; ++n) vw[n][w] &= keep;
             }
         }
-        float tmax = -kInf;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tmax = fmaxf(tmax, s[i][c]);
-        const float mn = fmaxf(m, group_max(tmax));
-        const float ms = mn == -kInf ? 0.0f : mn;
-        float alpha = exp2_fast(m - ms);
-        m = mn;
         // the value scales' reference: the largest so far, same in every lane
         const float vn = fmaxf(vref, group_max(vs));
         const float vr = vn > 0.0f ? 1.0f / vn : 0.0f;
         const float wf = vs * vr * kWeightScale;
-        l *= alpha;
-        f16x8 p[2];
+        f16x8 p[NQ][2];
+        float alpha[NQ];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int b = 0; b < NQ; ++b) {
+            float tmax = -kInf;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const float e = exp2_fast(s[i][c] - ms);
-                l += e;
-                p[i >> 1][4 * (i & 1) + c] = (_Float16)(e * wf);
-            }
-        alpha *= vref * vr;
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmax = fmaxf(tmax, s[b][i][c]);
+            const float mn = fmaxf(m[b], group_max(tmax));
+            const float ms = mn == -kInf ? 0.0f : mn;
+            alpha[b] = exp2_fast(m[b] - ms);
+            m[b] = mn;
+            l[b] *= alpha[b];
+            alpha[b] *= vref * vr;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const float e = exp2_fast(s[b][i][c] - ms);
+                    l[b] += e;
+                    p[b][i >> 1][4 * (i & 1) + c] = (_Float16)(e * wf);
+                }
+        }
         vref = vn;
 #pragma unroll
         for (int n = 0; n < ND; ++n) {
-            o[n] *= alpha;
-            o[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_f16<CODE>(vw[n][0], vw[n][1]),
-                                                          p[0], o[n], 0, 0, 0);
-            o[n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(codes_f16<CODE>(vw[n][2], vw[n][3]),
-                                                          p[1], o[n], 0, 0, 0);
+            const f16x8 v0 = codes_f16<CODE>(vw[n][0], vw[n][1]);
+            const f16x8 v1 = codes_f16<CODE>(vw[n][2], vw[n][3]);
+#pragma unroll
+            for (int b = 0; b < NQ; ++b) {
+                o[b][n] *= alpha[b];
+                o[b][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[b][0], o[b][n], 0, 0, 0);
+                o[b][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[b][1], o[b][n], 0, 0, 0);
+            }
         }
     }
 
-    // Join the waves: lane (col, g) holds channels 16 n + 4 g + c of row col.
-    l = group_sum(l);
+    // Join the waves, 16 rows at a time: lane (col, g) holds channels
+    // 16 n + 4 g + c of row col.
     const float of = vref * (1.0f / kWeightScale);
-    if (col < rows_max) {
-        if (g == 0) {
-            lds_ml[(wave * rows_max + col) * 2] = m;
-            lds_ml[(wave * rows_max + col) * 2 + 1] = l;
-        }
-        float *dst = lds + (wave * rows_max + col) * (D + 4) + 4 * g;
 #pragma unroll
-        for (int n = 0; n < ND; ++n) *reinterpret_cast<f32x4 *>(dst + 16 * n) = o[n] * of;
-    }
-    __syncthreads();
-    // 4 channels a thread
-    const int rows = r.n_rows - r.row0 < kFewTile ? r.n_rows - r.row0 : kFewTile;
-    for (int i = threadIdx.x; i < rows * (D / 4); i += 64 * NW) {
-        const int orow = i / (D / 4), d = i % (D / 4) * 4;
-        float mm = -kInf, ll = 0.0f;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) mm = fmaxf(mm, lds_ml[(w * rows_max + orow) * 2]);
-        const float ms = mm == -kInf ? 0.0f : mm;
-        f32x4 y = {0, 0, 0, 0};
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            const int at = w * rows_max + orow;
-            const float f = exp2_fast(lds_ml[at * 2] - ms);
-            ll += f * lds_ml[at * 2 + 1];
-            y += f * *reinterpret_cast<const f32x4 *>(lds + at * (D + 4) + d);
-        }
-        const RowPlace place = place_of(a, r.row0 + orow);
-        const int64_t at = (int64_t)(r.o0 + place.token) * a.n_heads + kvh * a.ratio +
-                           place.member;
-        if (alone && a.n_splits > 1 && d == 0) a.part_ml[2 * at + 1] = kAlone;
-        if (!alone) {
-            const int64_t part = (int64_t)split * a.batch.n_tokens * a.n_heads + at;
-            if (d == 0) {
-                a.part_ml[2 * part] = mm;
-                a.part_ml[2 * part + 1] = ll;
+    for (int b = 0; b < NQ; ++b) {
+        const float sum = group_sum(l[b]);
+        if (b > 0) __syncthreads();
+        if (col < rows_max) {
+            if (g == 0) {
+                lds_ml[(wave * rows_max + col) * 2] = m[b];
+                lds_ml[(wave * rows_max + col) * 2 + 1] = sum;
             }
-            if (te > tb) *reinterpret_cast<f32x4 *>(a.part_o + part * D + d) = y;
-            continue;
+            float *dst = lds + (wave * rows_max + col) * (D + 4) + 4 * g;
+#pragma unroll
+            for (int n = 0; n < ND; ++n) *reinterpret_cast<f32x4 *>(dst + 16 * n) = o[b][n] * of;
         }
-        y *= ll == 0.0f ? 0.0f : 1.0f / ll;
-        if (a.out_bf16)
-            *reinterpret_cast<u32x2v *>(static_cast<uint16_t *>(a.out) + at * D + d) =
-                u32x2v{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3])};
-        else
-            *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + at * D + d) = y;
+        __syncthreads();
+        // 4 channels a thread
+        const int row0 = r.row0 + 16 * b;
+        const int rows = r.n_rows - row0 < 16 ? r.n_rows - row0 : 16;
+        for (int i = threadIdx.x; i < rows * (D / 4); i += 64 * NW) {
+            const int orow = i / (D / 4), d = i % (D / 4) * 4;
+            float mm = -kInf, ll = 0.0f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) mm = fmaxf(mm, lds_ml[(w * rows_max + orow) * 2]);
+            const float ms = mm == -kInf ? 0.0f : mm;
+            f32x4 y = {0, 0, 0, 0};
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const int at = w * rows_max + orow;
+                const float f = exp2_fast(lds_ml[at * 2] - ms);
+                ll += f * lds_ml[at * 2 + 1];
+                y += f * *reinterpret_cast<const f32x4 *>(lds + at * (D + 4) + d);
+            }
+            const RowPlace place = place_of(a, row0 + orow);
+            const int64_t at = (int64_t)(r.o0 + place.token) * a.n_heads + kvh * a.ratio +
+                               place.member;
+            if (alone && a.n_splits > 1 && d == 0) a.part_ml[2 * at + 1] = kAlone;
+            if (!alone) {
+                const int64_t part = (int64_t)split * a.batch.n_tokens * a.n_heads + at;
+                if (d == 0) {
+                    a.part_ml[2 * part] = mm;
+                    a.part_ml[2 * part + 1] = ll;
+                }
+                if (te > tb) *reinterpret_cast<f32x4 *>(a.part_o + part * D + d) = y;
+                continue;
+            }
+            y *= ll == 0.0f ? 0.0f : 1.0f / ll;
+            if (a.out_bf16)
+                *reinterpret_cast<u32x2v *>(static_cast<uint16_t *>(a.out) + at * D + d) =
+                    u32x2v{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3])};
+            else
+                *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + at * D + d) = y;
+        }
     }
 }
 
@@ -337,23 +372,25 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Attend a)
 }
 
 template <int D, int CODE>
-hipError_t few_code(const Attend &a, int waves, hipStream_t stream)
+hipError_t few_code(const Attend &a, const AttendPlan &p, hipStream_t stream)
 {
-    const dim3 grid((unsigned)attend_row_tiles(a.batch, a.ratio, kFewTile), a.cache.n_kv_heads,
+    const dim3 grid((unsigned)attend_row_tiles(a.batch, a.ratio, p.tile), a.cache.n_kv_heads,
                     a.n_splits);
-    const unsigned bytes = few_lds(D, waves, a.lds_rows);
-    if (waves > 4)
-        attend_kernel<D, CODE, many_waves(D)><<<grid, 64 * many_waves(D), bytes, stream>>>(a);
+    const unsigned bytes = few_lds(D, p.waves, a.lds_rows);
+    if (p.waves > 4)
+        attend_kernel<D, CODE, many_waves(D), 1><<<grid, 64 * many_waves(D), bytes, stream>>>(a);
+    else if (p.tile == kWideTile)
+        attend_kernel<D, CODE, 4, D <= 128 ? 2 : 1><<<grid, 256, bytes, stream>>>(a);
     else
-        attend_kernel<D, CODE, 4><<<grid, 256, bytes, stream>>>(a);
+        attend_kernel<D, CODE, 4, 1><<<grid, 256, bytes, stream>>>(a);
     return hipGetLastError();
 }
 
 template <int D>
-hipError_t few_dim(const Attend &a, int waves, hipStream_t stream)
+hipError_t few_dim(const Attend &a, const AttendPlan &p, hipStream_t stream)
 {
-    return a.cache.code_type == RRQ_CODE_INT8 ? few_code<D, RRQ_CODE_INT8>(a, waves, stream)
-                                              : few_code<D, RRQ_CODE_FP8>(a, waves, stream);
+    return a.cache.code_type == RRQ_CODE_INT8 ? few_code<D, RRQ_CODE_INT8>(a, p, stream)
+                                              : few_code<D, RRQ_CODE_FP8>(a, p, stream);
 }
 
 template <int D>
@@ -374,18 +411,28 @@ AttendPlan attend_plan(const rrq_cache &c, const rrq_batch &b, int n_heads)
     const int ratio = n_heads / c.n_kv_heads;
     const int64_t cap = b.max_pages * c.page_size;      // longest sequence there can be
     AttendPlan p = {};
-    p.rows_form = b.n_tokens * ratio > kFewMaxRows * b.n_seqs;
-    const int64_t units = attend_row_tiles(b, ratio, p.rows_form ? kRowsTile : kFewTile) *
-                          c.n_kv_heads;
-    p.lds_rows = b.n_tokens * ratio < kFewTile ? (int)(b.n_tokens * ratio) : kFewTile;
+    const int64_t rows = b.n_tokens * ratio;
+    // The form by the rows a sequence and kv head (mean): this one reads and
+    // widens the codes once a row tile, the other once for 128 rows, but waits
+    // at a barrier each tile of keys. Measured at 16 sequences of 300 to 9000
+    // positions: 60 rows with heads of 64, 26.8 us here and 29.7 there; 40 rows
+    // with heads of 128, 56 and 50.5; with heads of 256, 124 and 92.
+    p.rows_form = rows > (c.head_dim == 64 ? 64 : 32) * b.n_seqs;
+    // Tiles of 32 rows halve the codes to widen (20 rows, heads of 128: 58 us;
+    // 75 in tiles of 16), but hold two rows' queries and outputs a lane: with
+    // heads of 256 that no longer fits the registers.
+    p.tile = p.rows_form ? kRowsTile
+                         : (rows > 16 * b.n_seqs && c.head_dim <= 128 ? kWideTile : 16);
+    const int64_t units = attend_row_tiles(b, ratio, p.tile) * c.n_kv_heads;
+    p.lds_rows = rows < 16 ? (int)rows : 16;
     p.waves = 4;
     p.splits = 1;
-    if (!p.rows_form && cap <= 2048 && units <= kServeCus &&
+    if (p.tile == 16 && cap <= 2048 && units <= kServeCus &&
         few_lds(c.head_dim, many_waves(c.head_dim), p.lds_rows) <= 65536) {
         p.waves = many_waves(c.head_dim);
         return p;
     }
-    p.target = p.rows_form ? 768 : 2048;
+    p.target = p.rows_form ? 768 : (p.tile == kWideTile ? 512 : 2048);
     p.min_tiles = p.rows_form && c.head_dim > 64 ? 16 : 8;
     if (units >= (p.rows_form ? 4 * kServeCus : p.target)) return p;
     const int64_t most = (cap + p.min_tiles * kTileKeys - 1) / (p.min_tiles * kTileKeys);
@@ -401,11 +448,11 @@ hipError_t launch_attend(const Attend &a, const AttendPlan &p, hipStream_t strea
     if (p.rows_form)
         e = launch_attend_rows(a, stream);
     else if (a.cache.head_dim == 64)
-        e = few_dim<64>(a, p.waves, stream);
+        e = few_dim<64>(a, p, stream);
     else if (a.cache.head_dim == 128)
-        e = few_dim<128>(a, p.waves, stream);
+        e = few_dim<128>(a, p, stream);
     else
-        e = few_dim<256>(a, p.waves, stream);
+        e = few_dim<256>(a, p, stream);
     if (e != hipSuccess || a.n_splits == 1) return e;
     if (a.cache.head_dim == 64) return join_dim<64>(a, stream);
     if (a.cache.head_dim == 128) return join_dim<128>(a, stream);

@@ -43,22 +43,20 @@ hipError_t launch_cache_read(const CacheRead &a, bool bf16, hipStream_t stream);
 
 // Attention. Rows of a sequence and kv head are (token, query head of the
 // group): row r is token r / ratio, head kv * ratio + r % ratio. Two forms: few
-// rows a sequence (row tiles of 16, rrq_attention.hip) and many (row tiles of
-// 128, rrq_attention_rows.hip). At most offsets[b + 1] * ratio / R - offsets[b]
+// rows a sequence (row tiles of 16 or 32, rrq_attention.hip) and many (row tiles
+// of 128, rrq_attention_rows.hip). At most offsets[b + 1] * ratio / R - offsets[b]
 // * ratio / R + 1 tiles of R rows hold a sequence's rows.
-constexpr int kFewTile = 16, kRowsTile = 128;
-// Rows a sequence (on average) up to which the few-row form serves a call.
-constexpr int64_t kFewMaxRows = 32;
+constexpr int kWideTile = 32, kRowsTile = 128;
 inline int64_t attend_row_tiles(const rrq_batch &b, int ratio, int tile)
 {
     return b.n_tokens * ratio / tile + b.n_seqs;
 }
-// How a call is served: the form; the key ranges a row tile is split into at
+// How a call is served: the form and its rows a tile; the key ranges a row tile is split into at
 // most, of min_tiles 64-key tiles at least, about target workgroups in all;
 // waves a workgroup and rows a tile of the few-row form.
 struct AttendPlan {
     bool rows_form;
-    int splits, target, min_tiles, waves, lds_rows;
+    int tile, splits, target, min_tiles, waves, lds_rows;
 };
 AttendPlan attend_plan(const rrq_cache &c, const rrq_batch &b, int n_heads);
 struct Attend {
