@@ -234,6 +234,7 @@ __global__ __launch_bounds__(64 * kWaves, 5) void logprobs_kernel(Logprobs a)
 {
     __shared__ key_t lds_keys[kWaves][kSlots];
     __shared__ float lds_sums[kWaves][3];
+    __shared__ uint32_t lds_nth[kWaves];
     constexpr int VEC = BF16 ? 8 : 4;           // logits a load
     constexpr int NV = kPerLane / VEC;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -245,6 +246,9 @@ __global__ __launch_bounds__(64 * kWaves, 5) void logprobs_kernel(Logprobs a)
     const uint32_t parts = a.segments * kWaves, blocks = (vocab + kBlock - 1) / kBlock;
     const uint32_t p = seg * kWaves + wave, each = blocks / parts, more = blocks % parts;
     const uint32_t b0 = each * p + (p < more ? p : more), b1 = b0 + each + (p < more ? 1 : 0);
+
+    // every wave of the workgroup has a block: their first ones share a floor
+    const bool shared = each > 0 || seg * kWaves + kWaves - 1 < more;
 
     Sums s = {-kInf, 0.0f, 0.0f};
     Top top = {lds_keys[wave], a.n_top, 0, 0};
@@ -302,10 +306,19 @@ __global__ __launch_bounds__(64 * kWaves, 5) void logprobs_kernel(Logprobs a)
         // a later block has higher indices: an equal logit does not matter
         const uint32_t bo = ordered(bm);
         if (top.floor != 0 && !__any(bo > (uint32_t)(top.floor >> 32))) continue;
-        // What n lanes' maxima reach is a floor that n logits reach. A maximum
+        // What n lanes' maxima reach is a floor that n logits reach; so is, in
+        // the first blocks, what ceil(n / 4) lanes of each wave reach. A maximum
         // of -inf counts if it is a logit's, not just where the lane began.
         const bool has = bm > -kInf || (at0 < vocab && v[0] == -kInf);
-        const uint32_t nth = nth_largest(has ? bo : 0, a.n_top);
+        const bool first = shared && b == b0;
+        uint32_t nth = nth_largest(has ? bo : 0,
+                                   first ? (a.n_top + kWaves - 1) / kWaves : a.n_top);
+        if (first) {
+            if (lane == 0) lds_nth[wave] = nth;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) nth = lds_nth[w] < nth ? lds_nth[w] : nth;
+        }
         const key_t least = ((key_t)nth << 32) - 1;
         if (nth > 0 && least > top.floor) top.floor = least;
         const float fv = top.floor_value();
@@ -421,7 +434,12 @@ int logprobs_segments(int64_t n_rows, int64_t vocab)
     const int64_t most = (vocab + kBlock * kWaves - 1) / (kBlock * kWaves);
     int64_t n = (kServeCus * 4 + n_rows - 1) / n_rows;
     n = n > most ? most : n;
-    return n < 1 ? 1 : (int)n;
+    if (n < 1) n = 1;
+    // and no more than the longest part needs: 96 rows of 150001 in 10 segments
+    // of two blocks a wave, not 11 with some waves at one (27.8 -> 26.9 us)
+    const int64_t blocks = (vocab + kBlock - 1) / kBlock;
+    const int64_t longest = (blocks + n * kWaves - 1) / (n * kWaves);
+    return (int)((blocks + longest * kWaves - 1) / (longest * kWaves));
 }
 
 size_t logprobs_row_bytes(int segments, int n_top)
