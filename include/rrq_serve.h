@@ -74,7 +74,7 @@ typedef struct rrq_cache {
  *               sequence's length reaches. A page that is written belongs to
  *               one sequence.
  *   lengths     device, int32 [n_seqs]: tokens of the sequence, this call's
- *               included.
+ *               included (below 0: none). Attention sees the first 2^31 - 4096.
  *   offsets     device, int32 [n_seqs + 1], ascending.
  *   table_stride, max_pages  1 <= max_pages <= table_stride.
  *   n_seqs      0..2^20 (0: the call enqueues nothing).

@@ -46,7 +46,7 @@ __device__ __forceinline__ bool find_rows(const Attend &a, int u, RowTile &r)
     r.seq = s;
     r.o0 = uniform(clamp_row(a.batch, s));
     const int n = uniform(clamp_row(a.batch, s + 1)) - r.o0;
-    const int len = uniform(a.batch.lengths[s]);
+    const int given = uniform(a.batch.lengths[s]), len = given < 0 ? 0 : given;
     r.row0 = (u - ((r.o0 * a.ratio >> shift) + s)) * R;
     r.n_rows = n * a.ratio;
     if (n <= 0 || r.row0 < 0 || r.row0 >= r.n_rows) return false;   // < 0: before the first sequence

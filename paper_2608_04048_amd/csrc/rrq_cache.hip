@@ -82,8 +82,8 @@ __device__ __forceinline__ float block_max(float a, float *lds)
 }
 
 // The block's scale from the new values' largest and the stored scale; inv
-// is its reciprocal and ratio the factor of the codes already there (0: they
-// stay).
+// is its reciprocal and ratio the factor of the codes already there (below 0:
+// they stay; 0 is a factor, of a scale that grew past binary32's range).
 template <int CODE>
 __device__ __forceinline__ float block_scale(float amax, float stored, float &inv, float &ratio)
 {
@@ -91,7 +91,7 @@ __device__ __forceinline__ float block_scale(float amax, float stored, float &in
     float s = fmaxf(stored, amax * c);
     if (s < 0x1p-126f) s = 0.0f;
     inv = s > 0.0f ? 1.0f / s : 0.0f;
-    ratio = s > stored && stored > 0.0f ? stored * inv : 0.0f;
+    ratio = s > stored && stored > 0.0f ? stored * inv : -1.0f;
     return s;
 }
 
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(1024) void cache_write_kernel(CacheWrite a)
             const int slot = slot0 + i * tokens;
             if (slot >= p.lo && slot < p.hi)
                 codes[slot * TPT + c] = encode4<CODE>(x[i] * inv);
-            else if (slot < p.lo && ratio > 0.0f)
+            else if (slot < p.lo && ratio >= 0.0f)
                 codes[slot * TPT + c] =
                     encode4<CODE>(codes_f32<CODE>(codes[slot * TPT + c]) * ratio);
         }
@@ -163,7 +163,7 @@ __global__ __launch_bounds__(1024) void cache_write_kernel(CacheWrite a)
         const float s = block_scale<CODE>(amax, stored, inv, ratio);
         const bool any = slot0 < p.hi && slot0 + kRun > p.lo;
         const bool whole = slot0 >= p.lo && slot0 + kRun <= p.hi;
-        const bool moves = slot0 < p.lo && ratio > 0.0f;
+        const bool moves = slot0 < p.lo && ratio >= 0.0f;
         if (active && (any || moves)) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -177,7 +177,7 @@ __global__ __launch_bounds__(1024) void cache_write_kernel(CacheWrite a)
                                      x[4 * q + 3][e]};
                     uint32_t v = encode4<CODE>(y * inv);
                     if (!whole) {
-                        const uint32_t kept = ratio > 0.0f
+                        const uint32_t kept = ratio >= 0.0f
                             ? encode4<CODE>(codes_f32<CODE>(old[q]) * ratio) : old[q];
                         uint32_t is_new = 0, is_kept = 0;
 #pragma unroll

@@ -58,6 +58,23 @@ def test_write_equals_the_definition(gpu, code, dtype, heads, dim, page):
 
 
 @pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_scale_that_grows_past_the_range_of_its_ratio(gpu, code, dtype):
+    """The stored scale over the new one is below every binary32: the kept
+    codes become zeros."""
+    import torch
+    seqs = [(1, 12), (4, 16), (2, 31)]
+    s = Setup(gpu, seqs, 2, 64, 16, code, seed=4).fill([length - n for n, length in seqs])
+    s.host.ks *= np.float32(1e-30)
+    s.host.vs *= np.float32(1e-30)
+    K = bf16(_rows(s.rng, s.offsets[-1], 2, 64) * np.float32(1e33))
+    V = bf16(_rows(s.rng, s.offsets[-1], 2, 64) * np.float32(1e34))
+    _check(s, K, V, torch.float32 if dtype == "f32" else torch.bfloat16)
+    page = s.host.block("k", s.table[0, 0], 0)
+    assert (page[:11] & 0x7F == 0).all()
+
+
+@pytest.mark.parametrize("code", CODES)
 @pytest.mark.parametrize("gain", [1e-3, 1.0, 37.0, 1e4])
 def test_a_growing_scale_moves_the_codes_already_there(gpu, code, gain):
     import torch
