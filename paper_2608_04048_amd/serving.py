@@ -422,7 +422,7 @@ def token_logprobs(logits, targets=None, n_top: int = 0, workspace=None, stream=
         target_ptr, logprob_ptr = targets.data_ptr(), logprobs.data_ptr()
     entropy = (torch.empty(rows, dtype=torch.float32, device=device) if logprobs is None else
                torch.empty_like(logprobs))
-    if n_top:
+    if n_top > 0:
         top_ids = torch.empty((rows, n_top), dtype=torch.int64, device=device)
         top_logprobs = torch.empty((rows, n_top), dtype=torch.float32, device=device)
         id_ptr, top_ptr = top_ids.data_ptr(), top_logprobs.data_ptr()
