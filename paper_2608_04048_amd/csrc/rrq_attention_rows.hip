@@ -317,23 +317,25 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
         const float ms = (m == -kInf ? 0.0f : m) - 6.0f;    // - 6: the weights' factor
         // vref / vs of the lane's run, and its log2. A block of zeros may take
         // any scale: vref's keeps w at the weight. Past 2^100 w is 0 in
-        // binary16 for any factor.
+        // binary16 for any factor (and weights down to 2^-26 of the largest
+        // still count in the sum).
         const float backs = vst > 0.0f ? fminf(vref * __builtin_amdgcn_rcpf(vst), 0x1p100f) : 1.0f;
         const float lbacks = __builtin_amdgcn_logf(backs);
         f16x8 p[RUNS];
 #pragma unroll
         for (int i = 0; i < RUNS; ++i) {
             const float back = lane_value(backs, i), sub = ms + lane_value(lbacks, i);
+            // summed before they are rounded: a run whose value scale is far
+            // below vref has weights that binary16 loses, and its full share
+            // of the sum
             float sum = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                p[i][e] = (_Float16)exp2_fast(
+            for (int e = 0; e < 8; ++e) {
+                const float w = exp2_fast(
                     __builtin_fmaf(s[i >> 1][8 * (i & 1) + e], c[i], -sub));
-            // the rounded weights, as the second product takes them
-            const f16x2 ones = {(_Float16)1.0f, (_Float16)1.0f};
-#pragma unroll
-            for (int e = 0; e < 8; e += 2)
-                sum = __builtin_amdgcn_fdot2(f16x2{p[i][e], p[i][e + 1]}, ones, sum, false);
+                p[i][e] = (_Float16)w;
+                sum += w;
+            }
             l += sum * back;
         }
         place = thread();

@@ -66,6 +66,21 @@ def test_windows_in_several_ranges(gpu, dim, window, rows):
     _run(s, 2, window=window, gain=1.5)
 
 
+@pytest.mark.parametrize("rows", [1, 24, 100])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("power", [-12, -25, -45, -100])
+def test_most_of_the_weight_on_small_values(gpu, rows, dim, power):
+    """All pages but one or two hold values 2^power below theirs: they add
+    little to the output, but their weights count in full."""
+    s = Setup(gpu, [(rows, 300), (rows, 120), (rows, 3000)], 1, dim, 16, "int8",
+              seed=rows + dim).fill()
+    for b, kept in enumerate(((7,), (0, 7), (40, 120))):
+        for j, page in enumerate(s.table[b]):
+            if page >= 0 and j not in kept:
+                s.host.vs[page] *= np.float32(2.0 ** power)
+    _run(s, 2)
+
+
 @pytest.mark.parametrize("rows", [1, 100])
 def test_a_strided_page_table(gpu, rows):
     s = Setup(gpu, [(rows, 3000), (rows, 200)], 1, 64, 16, "int8", seed=rows).fill()
