@@ -164,9 +164,11 @@ int rrq_cache_read(const rrq_cache *cache, const rrq_batch *batch, void *K_out, 
  *
  * Arithmetic: queries are rounded to 11 significant bits (bfloat16 ones are
  * exact) relative to their row's largest, codes are exact, products are
- * summed in binary32; the softmax is binary32, its weights are rounded to 11
- * bits relative to the largest before the second product. Results are
- * deterministic for one shape of call; they may differ in the last bits
+ * summed in binary32; the softmax's sum is binary32; its weights, each with
+ * its block's value scale, are rounded to 11 bits before the second product,
+ * and those below 2^-20 of the row's largest to 2^-31 of it. (Value scales of
+ * one sequence and head are taken to lie within a factor of 2^100 of each
+ * other; smaller ones count as at that distance.) Results are deterministic for one shape of call; they may differ in the last bits
  * between calls of another batch.
  *
  * Returns RRQ_OK, or RRQ_ERR_NULL / _ALIGN / _SHAPE / _DTYPE / _FORMAT /

@@ -166,6 +166,30 @@ __device__ __forceinline__ void load_query(const Attend &a, int64_t at, float (&
     }
 }
 
+// Value scales are taken relative to vref, the largest of a wave's first keys
+// that are not all zeros. One that passes it by more than kReferAgain makes it
+// move (so that exponents stay far from binary32's ends): m falls by the
+// logarithm of the step and the sum l, in units of 2^m, grows by it; outputs
+// stay, as value scale and m move alike. The step ends at 2^90, past which
+// l could overflow: what went before then counts 2^-90 of the new scale.
+constexpr float kReferAgain = 0x1p60f;
+__device__ __forceinline__ void refer(float vmax, float vref, float &m, float &l)
+{
+    if (vref == 0.0f) return;           // nothing but zeros so far
+    const float up = fminf(vmax / vref, 0x1p90f);
+    m -= __builtin_amdgcn_logf(up);
+    l *= up;
+}
+// vref / vs: what a weight that carries vs counts in the sum, 2^100 at most
+// (with kSumUnit, which undoes the weights' largest factor, a sum of 2^27 of
+// them is finite). A block of zeros (vs = 0) may take any scale: a small one,
+// which does not push the other blocks' weights down.
+constexpr float kSumUnit = 0x1p-14f;
+__device__ __forceinline__ float scale_back(float vs, float vref)
+{
+    return vs > 0.0f ? fminf(vref * __builtin_amdgcn_rcpf(vs), 0x1p100f) : 0x1p60f;
+}
+
 // Queries go to binary16 times `up`, a power of two that brings the row's
 // largest magnitude to [2^13, 2^14) (smaller values keep 11 bits down to
 // 2^-27 of it), with the sign of the softmax scale; products times qf >= 0 are

@@ -25,7 +25,7 @@ namespace {
 
 // Weights are scaled by 2^14 before rounding to binary16, whose normal range
 // then reaches 2^-28 below the largest weight.
-constexpr float kWeightScale = 0x1p14f;
+constexpr float kWeightBits = 14.0f;
 
 // Maximum over the four lane groups: the swaps exchange the second halves of
 // rows (of the wave) of one copy with the first of the other.
@@ -204,10 +204,16 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
                 for (int n = 0; n < ND; ++n) vw[n][w] &= keep;
             }
         }
-        // the value scales' reference: the largest so far, same in every lane
-        const float vn = fmaxf(vref, group_max(vs));
-        const float vr = vn > 0.0f ? 1.0f / vn : 0.0f;
-        const float wf = vs * vr * kWeightScale;
+        // A weight carries its value scale, relative to vref, and so does the
+        // maximum: m is the row's largest score + log2(vs / vref). The sum gets
+        // the scale back.
+        const float vmax = group_max(vs);
+        if (__any(vmax > vref * kReferAgain)) {
+#pragma unroll
+            for (int b = 0; b < NQ; ++b) refer(vmax, vref, m[b], l[b]);
+            vref = vmax;
+        }
+        const float back = scale_back(vs, vref), lback = __builtin_amdgcn_logf(back);
         f16x8 p[NQ][2];
         float alpha[NQ];
 #pragma unroll
@@ -217,22 +223,22 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmax = fmaxf(tmax, s[b][i][c]);
-            const float mn = fmaxf(m[b], group_max(tmax));
+            const float mn = fmaxf(m[b], group_max(tmax - lback));
             const float ms = mn == -kInf ? 0.0f : mn;
             alpha[b] = exp2_fast(m[b] - ms);
             m[b] = mn;
-            l[b] *= alpha[b];
-            alpha[b] *= vref * vr;
+            const float sub = ms + lback - kWeightBits;
+            float sum = 0.0f;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    const float e = exp2_fast(s[b][i][c] - ms);
-                    l[b] += e;
-                    p[b][i >> 1][4 * (i & 1) + c] = (_Float16)(e * wf);
+                    const float w = exp2_fast(s[b][i][c] - sub);
+                    sum += w;       // (before it is rounded: it may be below binary16)
+                    p[b][i >> 1][4 * (i & 1) + c] = (_Float16)w;
                 }
+            l[b] = l[b] * alpha[b] + sum * (back * kSumUnit);
         }
-        vref = vn;
 #pragma unroll
         for (int n = 0; n < ND; ++n) {
             const f16x8 v0 = codes_f16<CODE>(vw[n][0], vw[n][1]);
@@ -248,7 +254,6 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
 
     // Join the waves, 16 rows at a time: lane (col, g) holds channels
     // 16 n + 4 g + c of row col.
-    const float of = vref * (1.0f / kWeightScale);
 #pragma unroll
     for (int b = 0; b < NQ; ++b) {
         const float sum = group_sum(l[b]);
@@ -260,7 +265,7 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
             }
             float *dst = lds + (wave * rows_max + col) * (D + 4) + 4 * g;
 #pragma unroll
-            for (int n = 0; n < ND; ++n) *reinterpret_cast<f32x4 *>(dst + 16 * n) = o[b][n] * of;
+            for (int n = 0; n < ND; ++n) *reinterpret_cast<f32x4 *>(dst + 16 * n) = o[b][n] * kSumUnit * vref;
         }
         __syncthreads();
         // 4 channels a thread

@@ -11,10 +11,12 @@
 // 16-key runs are laid out in LDS in that order.
 //
 // Scales: a run of 16 keys lies in one page, so its key scale and value scale
-// are wave-uniform. The weights carry the value scale through the exponent,
-//   w = exp2(s c - m + lv),  c = key scale x query factor, lv = log2(vs / vref),
-// and the sum of the softmax gets it back once a run: l += (vref / vs) sum w.
-// vref is the largest value scale so far, so w <= 1 (times 2^8, below).
+// are wave-uniform. A weight carries its value scale through the exponent,
+//   w = exp2(s c + lv - m),  c = key scale x query factor, lv = log2(vs / vref),
+// with m the largest s c + lv: weights are relative to the row's largest
+// contribution, whatever the scales of other pages. The softmax's sum gets the
+// scale back once a run: l += (vref / vs) sum w. vref is a scale of the range
+// at hand that keeps the exponents small.
 //
 // The running maximum m moves only when a tile's exceeds it by 8 (weights
 // then grow to 2^8 at most): most tiles skip the output's rescaling.
@@ -287,6 +289,16 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
                         s[h][e] = -kInf;
                 }
         }
+        float vmax = lane_value(vst, 0);
+#pragma unroll
+        for (int i = 1; i < RUNS; ++i) vmax = maximum(vmax, lane_value(vst, i));
+        if (vmax > vref * kReferAgain) {
+            refer(vmax, vref, m, l);
+            vref = vmax;
+        }
+        // vref / vs of the lane's run, and its log2
+        const float backs = scale_back(vst, vref);
+        const float lbacks = __builtin_amdgcn_logf(backs), units = backs * kSumUnit;
         // c: factor of a run's products. 0 (a block of zeros) becomes the least
         // number, which leaves -inf as it is.
         float tmax = -kInf, c[RUNS];
@@ -297,37 +309,24 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
             float x = s[i >> 1][8 * (i & 1)];
 #pragma unroll
             for (int e = 1; e < 8; ++e) x = maximum(x, s[i >> 1][8 * (i & 1) + e]);
-            tmax = maximum(tmax, x * c[i]);
+            tmax = maximum(tmax, __builtin_fmaf(x, c[i], -lane_value(lbacks, i)));
         }
         tmax = other_half_max(tmax);
-        float vmax = lane_value(vst, 0);
-#pragma unroll
-        for (int i = 1; i < RUNS; ++i) vmax = maximum(vmax, lane_value(vst, i));
-        if (__any(tmax > m + kSlack) || vmax > vref) {
+        if (__any(tmax > m + kSlack)) {
             const float mn = fmaxf(m, tmax);
             const float alpha = mn == -kInf ? 0.0f : exp2_fast(m - mn);
             m = mn;
             l *= alpha;
-            const float vn = fmaxf(vref, vmax);
-            const float oa = vn > 0.0f ? alpha * (vref / vn) : 0.0f;
-            vref = vn;
 #pragma unroll
-            for (int n = 0; n < ND; ++n) o[n] *= oa;
+            for (int n = 0; n < ND; ++n) o[n] *= alpha;
         }
         const float ms = (m == -kInf ? 0.0f : m) - 6.0f;    // - 6: the weights' factor
-        // vref / vs of the lane's run, and its log2. A block of zeros may take
-        // any scale: vref's keeps w at the weight. Past 2^100 w is 0 in
-        // binary16 for any factor (and weights down to 2^-26 of the largest
-        // still count in the sum).
-        const float backs = vst > 0.0f ? fminf(vref * __builtin_amdgcn_rcpf(vst), 0x1p100f) : 1.0f;
-        const float lbacks = __builtin_amdgcn_logf(backs);
         f16x8 p[RUNS];
 #pragma unroll
         for (int i = 0; i < RUNS; ++i) {
-            const float back = lane_value(backs, i), sub = ms + lane_value(lbacks, i);
-            // summed before they are rounded: a run whose value scale is far
-            // below vref has weights that binary16 loses, and its full share
-            // of the sum
+            const float sub = ms + lane_value(lbacks, i);
+            // summed before they are rounded: binary16 loses the weights of a
+            // run of small values, which still has its full share of the sum
             float sum = 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -336,7 +335,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
                 p[i][e] = (_Float16)w;
                 sum += w;
             }
-            l += sum * back;
+            l += sum * lane_value(units, i);
         }
         place = thread();
         const uint8_t *vrows = buf + KB + (place & 31) * VROW + ((place >> 5) & 1) * 16;
@@ -351,7 +350,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
         barrier();
     }
 
-    // both l and o carry the weights' factor
+    // l and o carry the weights' factor, l in kSumUnit
     l += __shfl_xor(l, 32);
     if (!live) return;
     const int64_t at = (r.o0 + token) * a.n_heads + head;
@@ -369,10 +368,10 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
 #pragma unroll
             for (int g = 0; g < 4; ++g)
                 *reinterpret_cast<f32x4 *>(dst + 32 * n + 8 * g) =
-                    f32x4{o[n][4 * g], o[n][4 * g + 1], o[n][4 * g + 2], o[n][4 * g + 3]} * vref;
+                    f32x4{o[n][4 * g], o[n][4 * g + 1], o[n][4 * g + 2], o[n][4 * g + 3]} * kSumUnit * vref;
         return;
     }
-    const float norm = l == 0.0f ? 0.0f : vref / l;
+    const float norm = l == 0.0f ? 0.0f : vref * kSumUnit / l;
 #pragma unroll
     for (int n = 0; n < ND; ++n)
 #pragma unroll

@@ -81,6 +81,40 @@ def test_most_of_the_weight_on_small_values(gpu, rows, dim, power):
     _run(s, 2)
 
 
+@pytest.mark.parametrize("rows", [6, 100])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("powers", [(0, 30), (0, -40, 3, -20), (0, 65, 10), (-50, 30, -10, 60),
+                                    (-70, 0, 10), (None, 0), (None, -30, None, 5)])
+def test_rows_keep_their_precision_beside_larger_values(gpu, rows, dim, powers):
+    """Rows that see only a sequence's early pages, of small values, beside
+    rows of the same tile that see larger ones: each row within its own bound
+    (no share of the other rows' size). None: pages of zeros."""
+    s = Setup(gpu, [(rows, rows + 60), (rows, rows), (rows, 2500)], 1, dim, 16, "int8",
+              seed=rows + dim).fill()
+    for table in s.table:
+        for j, page in enumerate(table):
+            if page >= 0:
+                power = powers[j * len(powers) // max(len(table) // 20, 9) % len(powers)]
+                s.host.vs[page] *= np.float32(0 if power is None else 2.0 ** power)
+                if power is None:
+                    s.host.v[page] = 0
+    D, T = dim, s.offsets[-1]
+    Q = bf16(s.rng.normal(size=(T, 2, D)).astype(np.float32))
+    s.to_gpu()
+    got = s.rrq.cache_attention(s.cache, s.batch, s.torch.from_numpy(Q).cuda().bfloat16(),
+                                out_dtype=s.torch.float32).cpu().numpy()
+    want, mean_abs, reach = ora.attention(s.host, s.table, s.lengths, s.offsets, Q, D ** -0.5,
+                                          True, 0)
+    # _bound's terms without the largest row's: weights below the rounded form's
+    # normal range lose 2^-25 each, where the row's largest contribution has a
+    # weight of 2^6 at least (n keys: 127 n 2^-31 of its code, taken as over 64)
+    d = D ** -0.5 * reach * ((D + 8) * 2.0 ** -24 + 2.0 ** -22)
+    rel = np.expm1(2 * d) + 1.01 * 2.0 ** -11 + (max(s.lengths) + 64) * 2.0 ** -23
+    bound = rel[..., None] * mean_abs * (1 + 2.0 ** -23) + 2.0 ** -23 * np.abs(want) + 1e-37
+    far = np.abs(got - want) > bound + max(s.lengths) * 2.0 ** -30 * mean_abs.max(-1, keepdims=True)
+    assert not far.any(), (np.argwhere(far)[:4], (np.abs(got - want) / bound).max())
+
+
 @pytest.mark.parametrize("rows", [1, 100])
 def test_a_strided_page_table(gpu, rows):
     s = Setup(gpu, [(rows, 3000), (rows, 200)], 1, 64, 16, "int8", seed=rows).fill()
