@@ -411,10 +411,9 @@ hipError_t join_dim(const Attend &a, hipStream_t stream)
 
 }  // namespace
 
-AttendPlan attend_plan(const rrq_cache &c, const rrq_batch &b, int n_heads)
+AttendPlan attend_plan(const rrq_cache &c, const rrq_batch &b, int n_heads, int64_t window)
 {
     const int ratio = n_heads / c.n_kv_heads;
-    const int64_t cap = b.max_pages * c.page_size;      // longest sequence there can be
     AttendPlan p = {};
     const int64_t rows = b.n_tokens * ratio;
     // The form by the rows a sequence and kv head (mean): this one reads and
@@ -432,15 +431,43 @@ AttendPlan attend_plan(const rrq_cache &c, const rrq_batch &b, int n_heads)
     p.lds_rows = rows < 16 ? (int)rows : 16;
     p.waves = 4;
     p.splits = 1;
-    if (p.tile == 16 && cap <= 2048 && units <= kServeCus &&
-        few_lds(c.head_dim, many_waves(c.head_dim), p.lds_rows) <= 65536) {
-        p.waves = many_waves(c.head_dim);
+    // positions a row tile can reach over: the table's, or its window's (and one
+    // tile, as windows start anywhere)
+    int64_t reach = b.max_pages * c.page_size;
+    if (window > 0 && window < reach) {
+        const int64_t wide = window + p.tile / ratio + kTileKeys;
+        reach = wide < reach ? wide : reach;
+    }
+    // Few short sequences: one workgroup of many waves, two tiles a wave at most
+    // (one with heads of 256), saves the join's launch. One sequence: heads of
+    // 128, 1000 positions 12.0 us, 14.6 in ranges of 512; 2000 positions 17.7
+    // and 14.7; heads of 64, 2000 positions 11.7 and 13.5; heads of 256, 500
+    // positions 12.9 and 14.3, 1000 positions 20.6 and 18.6.
+    const int many = many_waves(c.head_dim);
+    const int64_t few_keys = many * kTileKeys * (c.head_dim == 256 ? 1 : 2);
+    if (p.tile == 16 && reach <= few_keys && units <= kServeCus &&
+        few_lds(c.head_dim, many, p.lds_rows) <= 65536) {
+        p.waves = many;
         return p;
     }
+    // Workgroups to aim at: as many as are resident of the 32-row tiles (two a
+    // compute unit) and of the 128-row tiles (three of heads of 64); four times
+    // that of the 16-row tiles, whose ranges are short against their spread.
+    // Three sequences of about 115000 positions, 16-row tiles: 143 us at 2048,
+    // 154 at 1024, 165 at 512. 16 sequences of 300 to 9000, 32-row tiles: 26 us
+    // at 512, 27.5 at 768, 33 at 1024; 128-row tiles (160 rows, heads of 128):
+    // 160 us at 768, 165 at 1024, 157 at 512, but 236, 244 and 253 on five
+    // chunks of 174 to 900 tokens.
     p.target = p.rows_form ? 768 : (p.tile == kWideTile ? 512 : 2048);
+    // The shortest ranges: 512 keys (32 sequences of 2000: 33 us; 35 at 256
+    // keys, 53 at 1024); 1024 where a range's outputs are 128 rows of 128 or 256
+    // channels (the five chunks, heads of 256, window 1024: 168 us at 512, 115
+    // whole).
     p.min_tiles = p.rows_form && c.head_dim > 64 ? 16 : 8;
     if (units >= (p.rows_form ? 4 * kServeCus : p.target)) return p;
-    const int64_t most = (cap + p.min_tiles * kTileKeys - 1) / (p.min_tiles * kTileKeys);
+    const int64_t least = p.min_tiles * kTileKeys;
+    if (reach <= least + least / 2) return p;       // split_tiles would leave it whole (120 us)
+    const int64_t most = (reach + least - 1) / least;
     int64_t n = 4 * p.target / units;
     n = n > most ? most : n;
     p.splits = n < 1 ? 1 : (n > 64 ? 64 : (int)n);

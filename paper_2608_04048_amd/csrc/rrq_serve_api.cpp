@@ -128,8 +128,9 @@ extern "C" int rrq_cache_attention_workspace(const rrq_cache *cache, const rrq_b
     if (st != RRQ_OK) return st;
     *workspace_bytes = 0;
     if (batch->n_seqs == 0 || batch->n_tokens == 0) return RRQ_OK;
+    // without a window: with one, no call takes more key ranges
     *workspace_bytes = attend_bytes(cache, batch, n_heads,
-                                    attend_plan(*cache, *batch, n_heads).splits);
+                                    attend_plan(*cache, *batch, n_heads, 0).splits);
     return RRQ_OK;
 }
 
@@ -164,7 +165,7 @@ extern "C" int rrq_cache_attention(const rrq_cache *cache, const rrq_batch *batc
     a.causal = causal;
     a.q_bf16 = q_dtype == RRQ_BF16;
     a.out_bf16 = out_dtype == RRQ_BF16;
-    const AttendPlan plan = attend_plan(*cache, *batch, n_heads);
+    const AttendPlan plan = attend_plan(*cache, *batch, n_heads, window);
     a.n_splits = plan.splits;
     a.target = plan.target;
     a.min_tiles = plan.min_tiles;

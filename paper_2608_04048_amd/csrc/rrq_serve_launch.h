@@ -58,7 +58,7 @@ struct AttendPlan {
     bool rows_form;
     int tile, splits, target, min_tiles, waves, lds_rows;
 };
-AttendPlan attend_plan(const rrq_cache &c, const rrq_batch &b, int n_heads);
+AttendPlan attend_plan(const rrq_cache &c, const rrq_batch &b, int n_heads, int64_t window);
 struct Attend {
     rrq_cache cache;
     rrq_batch batch;
