@@ -180,14 +180,15 @@ __device__ __forceinline__ void refer(float vmax, float vref, float &m, float &l
     m -= __builtin_amdgcn_logf(up);
     l *= up;
 }
-// vref / vs: what a weight that carries vs counts in the sum, 2^100 at most
-// (with kSumUnit, which undoes the weights' largest factor, a sum of 2^27 of
-// them is finite). A block of zeros (vs = 0) may take any scale: a small one,
-// which does not push the other blocks' weights down.
+// vref / vs: what a weight that carries vs counts in the sum, 2^100 at most, in
+// kSumUnit, which undoes the weights' largest factor (so a sum of 2^27 of them
+// is finite; the unit also shifts m, by a constant that falls out). A block of
+// zeros (vs = 0) may take any scale: a small one, which does not push the other
+// blocks' weights down.
 constexpr float kSumUnit = 0x1p-14f;
 __device__ __forceinline__ float scale_back(float vs, float vref)
 {
-    return vs > 0.0f ? fminf(vref * __builtin_amdgcn_rcpf(vs), 0x1p100f) : 0x1p60f;
+    return vs > 0.0f ? fminf(vref * kSumUnit * __builtin_amdgcn_rcpf(vs), 0x1p86f) : 0x1p46f;
 }
 
 // Queries go to binary16 times `up`, a power of two that brings the row's

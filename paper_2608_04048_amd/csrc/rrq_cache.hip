@@ -3,7 +3,13 @@
 //
 // One workgroup owns one page of one kv head and either its keys or its
 // values, so every code and the scale of the block have one writer and a
-// page that already holds tokens can be rescaled in place.
+// page that already holds tokens can be rescaled in place without atomics.
+//
+// Memory bounds long calls: per value 4 or 2 bytes in and 1 out, or the
+// reverse. 8713 bfloat16 tokens of seven prompts (8 kv heads of 128): write
+// 13.4 us (4.0 TB/s), read 12.2 us (4.4 TB/s); 130000 tokens read in 177 us (4.5
+// TB/s; a large device copy makes 4.67). The last tokens of 24 sequences: 5.2
+// and 4.5 us, a launch and one chain of dependent loads.
 #include "rrq_serve_device.h"
 #include "rrq_serve_launch.h"
 
@@ -95,9 +101,11 @@ __device__ __forceinline__ float block_scale(float amax, float stored, float &in
     return s;
 }
 
-// A thread holds 32 values: of the keys 4 channels of 8 tokens (16-byte loads
-// and 4-byte stores, both contiguous over the lanes), of the values 2
-// channels of a run of 16 tokens (the 16 codes of a channel are one store).
+// A thread holds 32 values, so that the block's maximum and its codes come from
+// one read: of the keys 4 channels of 8 tokens (16-byte loads and 4-byte stores,
+// both contiguous over the lanes), of the values 2 channels of a run of 16
+// tokens (the 16 codes of a channel are one store: the transposition happens in
+// registers).
 constexpr int kTok = 8, kRun = 16;
 
 template <int D, int CODE, bool BF16>

@@ -14,6 +14,12 @@
 // looked at again, about n log(N / n) keys of N in random order. A full
 // buffer is cut back to its best n by counting, for every key, the larger
 // ones.
+//
+// Long calls are bound by reading the logits: 2000 rows of 131072 in binary32,
+// 1.05 GB in 200 us (5.2 TB/s; a kernel that only reads makes 5.3). 96 rows of
+// 150001 in bfloat16 with 20 alternatives: 20 us and 6 of the join where the bytes
+// need 6; every wave has two blocks, so the selection's start is most of its 27
+// vector instructions a logit. One row of 131072: 8 + 4 us of latency.
 #include <hip/hip_runtime.h>
 
 #include "rrq_serve_device.h"
@@ -430,7 +436,9 @@ __global__ __launch_bounds__(64) void logprobs_join_kernel(Logprobs a)
 
 int logprobs_segments(int64_t n_rows, int64_t vocab)
 {
-    // four workgroups a compute unit, each wave at least one block
+    // four workgroups a compute unit, each wave at least one block: 300 rows of
+    // 131072 40 us (45 at two, 42 at eight), 96 of 150001 27 us (32, 28), 20 of
+    // 131072 16 us (17.5, 16)
     const int64_t most = (vocab + kBlock * kWaves - 1) / (kBlock * kWaves);
     int64_t n = (kServeCus * 4 + n_rows - 1) / n_rows;
     n = n > most ? most : n;
