@@ -128,7 +128,7 @@ __device__ __forceinline__ bool split_tiles(const Attend &a, int lo, int hi, int
         float share = batch_tiles<R>(a) * (float)a.cache.n_kv_heads / (float)a.target;
         share = fmaxf(share, (float)a.min_tiles);
         if ((float)tiles > 1.5f * share) {
-            const float want = ceilf((float)tiles / share);
+            const float want = floorf((float)tiles / share + 0.5f);
             n = want < (float)a.n_splits ? (int)want : a.n_splits;
             per = (int)((uint32_t)(tiles + n - 1) / (uint32_t)n);
         }

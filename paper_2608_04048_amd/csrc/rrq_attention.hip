@@ -428,7 +428,7 @@ AttendPlan attend_plan(const rrq_cache &c, const rrq_batch &b, int n_heads, int6
     // widens the codes once a row tile, the other once for 128 rows, but waits
     // at a barrier each tile of keys. Measured at 16 sequences of 300 to 9000
     // positions: 60 rows with heads of 64, 26.8 us here and 29.7 there; 40 rows
-    // with heads of 128, 56 and 50.5; with heads of 256, 124 and 92.
+    // with heads of 128, 58 and 49; with heads of 256, 125 and 84.
     p.rows_form = rows > (c.head_dim == 64 ? 64 : 32) * b.n_seqs;
     // Tiles of 32 rows halve the codes to widen (20 rows, heads of 128: 58 us;
     // 75 in tiles of 16), but hold two rows' queries and outputs a lane: with
@@ -458,20 +458,31 @@ AttendPlan attend_plan(const rrq_cache &c, const rrq_batch &b, int n_heads, int6
         p.waves = many;
         return p;
     }
-    // Workgroups to aim at: as many as are resident of the 32-row tiles (two a
-    // compute unit) and of the 128-row tiles (three of heads of 64); four times
-    // that of the 16-row tiles, whose ranges are short against their spread.
-    // Three sequences of about 115000 positions, 16-row tiles: 143 us at 2048,
-    // 154 at 1024, 165 at 512. 16 sequences of 300 to 9000, 32-row tiles: 26 us
-    // at 512, 27.5 at 768, 33 at 1024; 128-row tiles (160 rows, heads of 128):
-    // 160 us at 768, 165 at 1024, 157 at 512, but 236, 244 and 253 on five
-    // chunks of 174 to 900 tokens.
-    p.target = p.rows_form ? 768 : (p.tile == kWideTile ? 512 : 2048);
-    // The shortest ranges: 512 keys (32 sequences of 2000: 33 us; 35 at 256
-    // keys, 53 at 1024); 1024 where a range's outputs are 128 rows of 128 or 256
-    // channels (the five chunks, heads of 256, window 1024: 168 us at 512, 115
-    // whole).
-    p.min_tiles = p.rows_form && c.head_dim > 64 ? 16 : 8;
+    // Workgroups to aim at and the shortest ranges.
+    // 16-row tiles: three times what is resident, as lengths differ; 512 keys.
+    // Three sequences of about 115000 positions: 143 us at 2048 workgroups, 154 at
+    // 1024, 165 at 512; 32 sequences of 2000: 33 us in ranges of 512 keys, 35 of
+    // 256, 53 of 1024.
+    // 32-row tiles: what is resident (16 sequences of 300 to 9000 positions, heads
+    // of 64: 26 us at 512, 27.5 at 768, 33 at 1024).
+    // 128-row tiles, whose ranges cost a written and joined output of 128 rows:
+    // 1.5 a compute unit of 256 keys at least where the row tiles alone do not
+    // fill the card (a second round of workgroups would cost more than it
+    // shares out), else 768 of 1024 keys. In us, the two rules in this order:
+    // 300 rows x 4 on 2000 positions, heads of 128, 37.6 and 41.8; 40 x 4 on
+    // 900, 18.9 and 30.4; 16 sequences of 300 to 9000 with 160 rows, 146 and
+    // 160; five chunks of 174 to 900 tokens (over 256 row tiles), heads of 128,
+    // 251 and 238, heads of 256 and a window of 1024, 111 and 107. Heads of 64, three
+    // workgroups resident a compute unit, ranges of 512 keys: 4800 rows on 3000
+    // positions 35, and 43 of 256 keys.
+    const bool full = units > kServeCus + kServeCus / 4;
+    if (p.rows_form) {
+        p.target = c.head_dim == 64 ? 640 : (full ? 768 : 384);
+        p.min_tiles = c.head_dim == 64 ? 8 : (full ? 16 : 4);
+    } else {
+        p.target = p.tile == kWideTile ? 512 : 2048;
+        p.min_tiles = 8;
+    }
     if (units >= (p.rows_form ? 4 * kServeCus : p.target)) return p;
     const int64_t least = p.min_tiles * kTileKeys;
     if (reach <= least + least / 2) return p;       // split_tiles would leave it whole (120 us)
