@@ -181,3 +181,18 @@ def test_row_offsets_pass_32_bits(gpu):
     want = ora.token_logprobs(last, np.array([vocab - 1]), 2)
     assert abs(lp[-1].item() - want[0][0]) < 1e-4 and ids[-1].tolist() == [11, vocab - 1]
     assert ids[0].tolist() == [0, 1] and abs(lp[0].item() + np.log(vocab)) < 1e-4
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [3, 4, 5, 8, 9, 11, 2003, 4097, 6143, 6144, 6145, 8195])
+def test_ends_of_rows(gpu, dtype, vocab):
+    """A row's last block, for rows of less than one block a wave too; what
+    lies past a row's end is not a logit."""
+    rng = np.random.default_rng(vocab)
+    x = _logits(rng, 37, vocab, dtype)
+    x[5] = x[5, 0]
+    x[6, -1] = 60.0
+    x[7, :-1] = -np.inf
+    t = rng.integers(0, vocab, 37)
+    for n_top in (0, min(3, vocab), min(32, vocab)):
+        _check(gpu, x, t, n_top, dtype, vocab + 3)
