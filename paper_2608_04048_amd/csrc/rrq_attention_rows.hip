@@ -23,7 +23,7 @@
 // of the library makes 1133; the matrix cores are busy 41% of the cycles. A wave
 // waits for its LDS operands and the softmax between its two products; two
 // workgroups a compute unit (LDS and registers hold no more) overlap. Five
-// chunks of 174 to 900 tokens, heads of 256, window 1024: 44 GFLOP in 115 us (386
+// chunks of 174 to 900 tokens, heads of 256, window 1024: 44 GFLOP in 106 us (420
 // TFLOP/s): 340 row tiles on 256 compute units, and 32-key tiles, as LDS holds
 // two workgroups' 64-key tiles of such heads no more (one a compute unit: 156 us).
 //
