@@ -193,3 +193,69 @@ def test_refusals_of_tensors(gpu):
             call()
     # nothing was enqueued: the stream still works
     assert (r.cache_attention(s.cache, s.batch, Q) != 55).all()
+
+
+@pytest.mark.parametrize("rows", [1, 20, 90])
+def test_cache_offsets_pass_32_bits(gpu, rows):
+    """Pages past 4 GiB of codes (keys and values each) give what the same
+    pages give at the start of a small cache."""
+    import torch
+    s = Setup(gpu, [(rows, 700), (rows, 2000)], 8, 128, 128, "int8", seed=rows).fill().to_gpu()
+    Q = torch.randn((s.offsets[-1], 8, 128), device="cuda")
+    want = s.rrq.cache_attention(s.cache, s.batch, Q)
+    used = s.host.k.shape[0]
+    far = 36000
+    big = s.rrq.KVCache.empty(far + used, 8, 128, 128, "int8")
+    assert big.k_codes[:far].numel() > 2 ** 32
+    big.k_codes[far:], big.v_codes[far:] = s.k, s.v
+    big.k_scales[far:], big.v_scales[far:] = s.ks, s.vs
+    batch = s.rrq.CacheBatch(s.batch.page_table + far, s.batch.lengths, s.batch.offsets,
+                             s.offsets[-1])
+    assert torch.equal(s.rrq.cache_attention(big, batch, Q), want)
+
+
+@pytest.mark.parametrize("rows", [1, 20, 200])
+def test_a_captured_call_with_ranges(gpu, rows):
+    """Write, attention over several ranges and scoring in one graph, replayed
+    as lengths change, with eager work and synchronisation between."""
+    import torch
+    s = Setup(gpu, [(rows, 5000), (rows, 3000)], 1, 128, 64, "fp8", seed=rows).fill().to_gpu()
+    T = s.offsets[-1]
+    K = torch.empty((T, 1, 128), device="cuda")
+    Q = torch.empty((T, 4, 128), device="cuda")
+    logits = torch.empty((T, 20000), device="cuda")
+    targets = torch.arange(T, device="cuda")
+    out = torch.empty((T, 4, 128), device="cuda", dtype=torch.bfloat16)
+    w = s.rrq.attention_workspace(s.cache, s.batch, 4)
+    assert w is not None
+    wl = s.rrq.logprobs_workspace(logits, 6)
+
+    def step():
+        s.rrq.cache_write(s.cache, s.batch, K, K)
+        s.rrq.cache_attention(s.cache, s.batch, Q, workspace=w, out=out)
+        return s.rrq.token_logprobs(logits, targets, 6, workspace=wl)
+
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+
+    def fill():
+        for t in (K, Q, logits):
+            t.normal_(generator=g)
+
+    fill()
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step()
+    for first, second in ((5000, 300), (4000, 2900), (rows, 3000), (4999, rows)):
+        s.batch.lengths.copy_(torch.tensor([first, second], dtype=torch.int32))
+        fill()
+        graph.replay()
+        got = [out.clone()] + [t.clone() for t in captured]
+        torch.cuda.synchronize()
+        want = step()               # the same tokens again: the same codes
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], out)
+        for a, b in zip(got[1:], want):
+            assert torch.equal(a, b)
