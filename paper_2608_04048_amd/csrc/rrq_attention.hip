@@ -428,13 +428,18 @@ AttendPlan attend_plan(const rrq_cache &c, const rrq_batch &b, int n_heads, int6
     // widens the codes once a row tile, the other once for 128 rows, but waits
     // at a barrier each tile of keys. Measured at 16 sequences of 300 to 9000
     // positions: 60 rows with heads of 64, 26.8 us here and 29.7 there; 40 rows
-    // with heads of 128, 58 and 49; with heads of 256, 125 and 84.
-    p.rows_form = rows > (c.head_dim == 64 ? 64 : 32) * b.n_seqs;
+    // with heads of 128, 58 and 49; with heads of 256, 125 and 84. Where there are
+    // few row tiles, time is latency and this form ahead: 160 rows on 900
+    // positions, 8 kv heads of 128, 17.3 and 19.0; 84 rows of 4 sequences of 2000,
+    // 2 kv heads of 64, 13.3 and 20.4; 240 rows on 3000, 2 of 256, 20.9 and 33.9
+    // (but 120 rows on 30000, 2 of 256, 58 and 51).
     // Tiles of 32 rows halve the codes to widen (20 rows, heads of 128: 58 us;
     // 75 in tiles of 16), but hold two rows' queries and outputs a lane: with
     // heads of 256 that no longer fits the registers.
-    p.tile = p.rows_form ? kRowsTile
-                         : (rows > 16 * b.n_seqs && c.head_dim <= 128 ? kWideTile : 16);
+    p.tile = rows > 16 * b.n_seqs && c.head_dim <= 128 ? kWideTile : 16;
+    p.rows_form = rows > (c.head_dim == 64 ? 64 : 32) * b.n_seqs &&
+                  attend_row_tiles(b, ratio, p.tile) * c.n_kv_heads > kServeCus / 4;
+    if (p.rows_form) p.tile = kRowsTile;
     const int64_t units = attend_row_tiles(b, ratio, p.tile) * c.n_kv_heads;
     p.lds_rows = rows < 16 ? (int)rows : 16;
     p.waves = 4;
