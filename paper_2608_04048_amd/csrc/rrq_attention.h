@@ -198,7 +198,7 @@ __device__ __forceinline__ float scale_back(float vs, float vref)
 __device__ __forceinline__ void query_factors(const Attend &a, float amax, float &up, float &qf)
 {
     int e = (int)(__float_as_uint(amax) >> 23) - 127;
-    e = e < -100 ? -100 : (e > 120 ? 120 : e);
+    e = e < -100 ? -100 : (e > 127 ? 127 : e);
     up = __uint_as_float((uint32_t)(13 - e + 127) << 23);
     if (a.scale < 0.0f) up = -up;
     qf = __uint_as_float((uint32_t)(e - 13 + 127) << 23) * (fabsf(a.scale) * kLog2e);

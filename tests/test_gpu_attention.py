@@ -157,6 +157,14 @@ def test_query_ranges(gpu, gain):
     _run(s, 3, q="f32", gain=gain, scale=0.09 / gain)
 
 
+@pytest.mark.parametrize("heads", [(3, 1), (8, 8)])
+def test_queries_at_the_end_of_their_range(gpu, heads):
+    # up to 2e37, past 2^16 times 2^107
+    n, kv = heads
+    s = Setup(gpu, [(100, 150), (130, 190)], kv, 128, 32, "fp8", seed=50).fill()
+    _run(s, n, q="f32", gain=5e36, scale=0.09 / 5e36)
+
+
 def test_zero_queries(gpu):
     s = Setup(gpu, [(2, 150)], 1, 128, 32, "int8", seed=48).fill()
     _run(s, 3, gain=0.0)
