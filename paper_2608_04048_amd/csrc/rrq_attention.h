@@ -140,6 +140,20 @@ __device__ __forceinline__ bool split_tiles(const Attend &a, int lo, int hi, int
     return n == 1;
 }
 
+// What a range without keys leaves for the join: a sum of 0, no output. Grids
+// are as deep as the longest sequence may need, so most workgroups of a ragged
+// batch end here; they load no queries and pass no barrier.
+template <int R>
+__device__ __forceinline__ void empty_range(const Attend &a, const RowTile &r, int kvh, int split)
+{
+    const int row = r.row0 + (int)threadIdx.x;
+    if (threadIdx.x >= R || row >= r.n_rows) return;
+    const RowPlace place = place_of(a, row);
+    const int64_t at = (int64_t)(r.o0 + place.token) * a.n_heads + kvh * a.ratio + place.member;
+    const int64_t part = (int64_t)split * a.batch.n_tokens * a.n_heads + at;
+    *reinterpret_cast<f32x2 *>(a.part_ml + 2 * part) = f32x2{-kInf, 0.0f};
+}
+
 // N query values of the element offset `at` on.
 template <int N>
 __device__ __forceinline__ void load_query(const Attend &a, int64_t at, float (&x)[N])

@@ -84,6 +84,10 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
     tile_keys<R>(a, r, lo_any, hi_any, lo_all, hi_all);
     const bool alone = split_tiles<R>(a, lo_any, hi_any, split, tb, te);
     if (alone && split > 0) return;
+    if (!alone && te <= tb) {
+        empty_range<R>(a, r, kvh, split);
+        return;
+    }
 
     const int P = a.cache.page_size, H = a.cache.n_kv_heads;
     const int shift = __builtin_ctz(P);
@@ -303,7 +307,7 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
                     a.part_ml[2 * part] = mm;
                     a.part_ml[2 * part + 1] = ll;
                 }
-                if (te > tb) *reinterpret_cast<f32x4 *>(a.part_o + part * D + d) = y;
+                *reinterpret_cast<f32x4 *>(a.part_o + part * D + d) = y;
                 continue;
             }
             y *= ll == 0.0f ? 0.0f : 1.0f / ll;

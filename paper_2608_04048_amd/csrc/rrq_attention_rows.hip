@@ -105,6 +105,10 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
     int tb, te;
     const bool alone = split_tiles<R>(a, lo_any, hi_any, blockIdx.y, tb, te);
     if (alone && blockIdx.y > 0) return;
+    if (!alone && te <= tb) {
+        empty_range<R>(a, r, kvh, blockIdx.y);
+        return;
+    }
     tb *= kTileKeys / KEYS;                 // to tiles of KEYS
     te *= kTileKeys / KEYS;
     const int32_t *table = a.batch.page_table + r.seq * a.batch.table_stride;
@@ -370,7 +374,6 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
             a.part_ml[2 * part] = m;
             a.part_ml[2 * part + 1] = l;
         }
-        if (te <= tb) return;
         float *dst = a.part_o + part * D + 4 * hb;
 #pragma unroll
         for (int n = 0; n < ND; ++n)
