@@ -20,12 +20,15 @@
 // binary16): the key scale multiplies the product, the value scale the weight.
 //
 // Measured (keys and values in 8 bits, 8 kv heads of 128): a step of 64
-// sequences of 90 to 12000 positions, 40 query heads, 796 MB in 164 us and 6 of
+// sequences of 90 to 12000 positions, 40 query heads, 796 MB in 163 us and 6 of
 // the join (4.7 TB/s; a device copy makes 4.67, a kernel that only reads 5.3); a
 // step of three of 99000 to 131072, 749 MB in 137 + 5 us (5.3 TB/s). One sequence
 // of 1000 positions: 11.5 us, the latency of two tiles a wave on 8 compute units.
-// 16 sequences of 300 to 9000 with 60 rows each, 2 kv heads of 64: 21.7 + 4 us,
-// half of it the issue of vector instructions (softmax and widening).
+// 16 sequences of 300 to 9000 with 60 rows each, 2 kv heads of 64: 19.5 + 4 us,
+// some 40% of it the issue of vector instructions (softmax and widening), the
+// rest memory latency: two or three tiles a wave. Loading a tile's keys under
+// the softmax of the one before gains 1% there and makes the step of 64
+// sequences 186 us (fewer waves a SIMD, the last tile read twice).
 #include "rrq_attention.h"
 
 namespace rrq_detail {
@@ -473,7 +476,7 @@ AttendPlan attend_plan(const rrq_cache &c, const rrq_batch &b, int n_heads, int6
     // 1024, 165 at 512; 32 sequences of 2000: 33 us in ranges of 512 keys, 35 of
     // 256, 53 of 1024.
     // 32-row tiles: what is resident (16 sequences of 300 to 9000 positions, heads
-    // of 64: 26 us at 512, 27.5 at 768, 33 at 1024).
+    // of 64: 23.3 us at 512, 25.7 at 768).
     // 128-row tiles, whose ranges cost a written and joined output of 128 rows:
     // 1.5 a compute unit of 256 keys at least where the row tiles alone do not
     // fill the card (a second round of workgroups would cost more than it
