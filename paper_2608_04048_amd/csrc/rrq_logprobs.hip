@@ -37,10 +37,11 @@ constexpr int kBuffer = 128;            // keys a wave buffers
 constexpr int kSlots = kBuffer + 8;     // and what a cut pads them with
 typedef unsigned long long key_t;
 
-// Ascending order of floats as unsigned; NaN first.
+// Ascending order of floats as unsigned; NaN first. The two zeros are equal:
+// -0 + 0 is +0, and the sum is every other number itself.
 __device__ __forceinline__ uint32_t ordered(float x)
 {
-    const uint32_t b = __float_as_uint(x);
+    const uint32_t b = __float_as_uint(x + 0.0f);
     if (x != x) return 0;
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
