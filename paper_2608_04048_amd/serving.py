@@ -16,6 +16,11 @@ Every computation runs in the HIP kernels.
 A ``KVCache`` and a ``CacheBatch`` keep the tensors they were made of and a C
 descriptor of them; a program makes them once and updates the tensors in place
 (``lengths`` on the device from step to step).
+
+``stream`` (a torch stream or a raw handle; by default torch's current stream) is
+where a call allocates and works. The caller orders it after the work that made
+the inputs, and orders the use of the outputs after it; the tensors themselves
+may be let go at once.
 """
 
 from __future__ import annotations
@@ -27,6 +32,7 @@ import torch
 
 from . import (RRQ_BF16, RRQ_F32, RRQ_OK, RRQError, _check_device_tensor, _ptr, _stream,
                load_library)
+from .placement import on_stream
 
 RRQ_CODE_INT8 = 0
 RRQ_CODE_FP8 = 1
@@ -172,6 +178,7 @@ class KVCache:
         self.n_pages, self.n_kv_heads, self.page_size, self.head_dim = pages, heads, page, dim
         self.device = k_codes.device
         self.index = k_codes.get_device()
+        self.tensors = (k_codes, v_codes, k_scales, v_scales)
         self.desc = RrqCache(_ptr(k_codes), _ptr(v_codes), _ptr(k_scales), _ptr(v_scales), pages,
                              heads, dim, page, CODE_TYPES[code_type])
         self.ref = ctypes.byref(self.desc)
@@ -219,6 +226,7 @@ class CacheBatch:
         self.n_seqs, self.max_pages, self.n_tokens = n_seqs, max_pages, int(n_tokens)
         self.device = page_table.device
         self.index = page_table.get_device()
+        self.tensors = (page_table, lengths, offsets)
         self.workspace_bytes = {}       # by the cache's sizes and the head count
         self.desc = RrqBatch(_ptr(page_table), _ptr(lengths), _ptr(offsets), stride, max_pages,
                              n_seqs, self.n_tokens)
@@ -259,16 +267,6 @@ def _check_out(out, name, shape, dtype, index):
                          f"on {out.device}")
 
 
-def _used_on(stream, *tensors) -> None:
-    """Memory allocated here for the current stream that a kernel on another
-    stream uses must not be handed out again before that kernel is done."""
-    if isinstance(stream, int):
-        stream = torch.cuda.ExternalStream(stream)
-    for t in tensors:
-        if t is not None:
-            t.record_stream(stream)
-
-
 def _device_index(cache, batch) -> int:
     if cache.index != batch.index:
         raise ValueError(f"cache and batch must be on one device, got cuda:{cache.index} and "
@@ -281,6 +279,9 @@ def cache_write(cache: KVCache, batch: CacheBatch, K, V, stream=None) -> None:
     bfloat16, any token and head strides of whole 16 bytes) into the batch's
     pages."""
     index = _device_index(cache, batch)
+    if stream is not None:
+        with on_stream(index, stream, *cache.tensors, *batch.tensors, K, V):
+            return cache_write(cache, batch, K, V)
     rows, heads, dim = batch.n_tokens, cache.n_kv_heads, cache.head_dim
     kt, kh = _row_strides(K, "K", rows, heads, dim, index)
     vt, vh = _row_strides(V, "V", rows, heads, dim, index)
@@ -288,7 +289,7 @@ def cache_write(cache: KVCache, batch: CacheBatch, K, V, stream=None) -> None:
         raise TypeError(f"K and V must have one dtype, got {K.dtype} and {V.dtype}")
     st = (_lib or _library()).rrq_cache_write(cache.ref, batch.ref, K.data_ptr(), V.data_ptr(),
                                               _dtype_code(K.dtype, "K"), kt, kh, vt, vh,
-                                              _stream(stream))
+                                              _stream(None))
     if st != RRQ_OK:
         raise RRQError(st, "rrq_cache_write")
 
@@ -297,14 +298,16 @@ def cache_read(cache: KVCache, batch: CacheBatch, dtype=None, stream=None, out=N
     """(K, V) [n_tokens, n_kv_heads, head_dim] of the batch's tokens, dequantised
     to float32 or bfloat16 (the default). ``out`` may pass the pair."""
     index = _device_index(cache, batch)
+    if stream is not None:
+        used = (*cache.tensors, *batch.tensors, *(() if out is None else out))
+        with on_stream(index, stream, *used) as there:
+            return there.returned(cache_read(cache, batch, dtype, out=out))
     shape = (batch.n_tokens, cache.n_kv_heads, cache.head_dim)
     if out is None:
         dtype = torch.bfloat16 if dtype is None else dtype
         code = _dtype_code(dtype, "dtype")
         K = torch.empty(shape, dtype=dtype, device=cache.device)
         V = torch.empty_like(K)         # (quicker)
-        if stream is not None:
-            _used_on(stream, K, V)
     else:
         K, V = out
         dtype = K.dtype if dtype is None else dtype
@@ -312,19 +315,14 @@ def cache_read(cache: KVCache, batch: CacheBatch, dtype=None, stream=None, out=N
         _check_out(K, "out[0]", shape, dtype, index)
         _check_out(V, "out[1]", shape, dtype, index)
     st = (_lib or _library()).rrq_cache_read(cache.ref, batch.ref, K.data_ptr(), V.data_ptr(),
-                                             code, _stream(stream))
+                                             code, _stream(None))
     if st != RRQ_OK:
         raise RRQError(st, "rrq_cache_read")
     return K, V
 
 
-def _workspace(n_bytes: int, device, stream):
-    if n_bytes == 0:
-        return None
-    w = torch.empty(n_bytes, dtype=torch.uint8, device=device)
-    if stream is not None:
-        _used_on(stream, w)
-    return w
+def _workspace(n_bytes: int, device):
+    return torch.empty(n_bytes, dtype=torch.uint8, device=device) if n_bytes else None
 
 
 def _workspace_args(w, index: int):
@@ -349,9 +347,9 @@ def _attention_bytes(cache, batch, n_heads: int) -> int:
 
 def attention_workspace(cache: KVCache, batch: CacheBatch, n_heads: int):
     """A workspace for cache_attention on this cache, batch and head count
-    (uint8 tensor, or None if none is needed). Calls that may run at the same
-    time need their own."""
-    return _workspace(_attention_bytes(cache, batch, n_heads), cache.device, None)
+    (uint8 tensor, or None if none is needed; allocated, like any tensor, for the
+    current stream). Calls that may run at the same time need their own."""
+    return _workspace(_attention_bytes(cache, batch, n_heads), cache.device)
 
 
 def cache_attention(cache: KVCache, batch: CacheBatch, Q, scale=None, causal: bool = True,
@@ -360,6 +358,10 @@ def cache_attention(cache: KVCache, batch: CacheBatch, Q, scale=None, causal: bo
     over the batch's sequences: [n_tokens, n_heads, head_dim] in bfloat16 (the
     default) or float32. scale defaults to head_dim ** -0.5; window 0 is none."""
     index = _device_index(cache, batch)
+    if stream is not None:
+        with on_stream(index, stream, *cache.tensors, *batch.tensors, Q, workspace, out) as there:
+            return there.returned(cache_attention(cache, batch, Q, scale, causal, window,
+                                                  out_dtype, workspace, out=out))
     dim = cache.head_dim
     qt, qh = _row_strides(Q, "Q", batch.n_tokens, None, dim, index)
     shape = Q.shape
@@ -368,19 +370,17 @@ def cache_attention(cache: KVCache, batch: CacheBatch, Q, scale=None, causal: bo
         out_dtype = torch.bfloat16 if out_dtype is None else out_dtype
         out_code = _dtype_code(out_dtype, "out_dtype")
         out = torch.empty(shape, dtype=out_dtype, device=cache.device)
-        if stream is not None:
-            _used_on(stream, out)
     else:
         out_dtype = out.dtype if out_dtype is None else out_dtype
         out_code = _dtype_code(out_dtype, "out")
         _check_out(out, "out", shape, out_dtype, index)
     if workspace is None:
-        workspace = _workspace(_attention_bytes(cache, batch, n_heads), cache.device, stream)
+        workspace = _workspace(_attention_bytes(cache, batch, n_heads), cache.device)
     w, w_bytes = _workspace_args(workspace, index)
     st = (_lib or _library()).rrq_cache_attention(
         cache.ref, batch.ref, Q.data_ptr(), _dtype_code(Q.dtype, "Q"), qt, qh, n_heads,
         1.0 / math.sqrt(dim) if scale is None else scale, 1 if causal else 0, window,
-        out.data_ptr(), out_code, w, w_bytes, _stream(stream))
+        out.data_ptr(), out_code, w, w_bytes, _stream(None))
     if st != RRQ_OK:
         raise RRQError(st, "rrq_cache_attention")
     return out
@@ -390,7 +390,7 @@ def logprobs_workspace(logits, n_top: int = 0):
     """A workspace for token_logprobs on logits of this shape (uint8 tensor, or
     None if none is needed). Calls that may run at the same time need their own."""
     return _workspace(rrq_token_logprobs_workspace(logits.shape[0], logits.shape[1], n_top),
-                      logits.device, None)
+                      logits.device)
 
 
 def token_logprobs(logits, targets=None, n_top: int = 0, workspace=None, stream=None):
@@ -404,6 +404,9 @@ def token_logprobs(logits, targets=None, n_top: int = 0, workspace=None, stream=
     index = logits.get_device()
     if index < 0:
         raise ValueError(f"logits must be on a GPU device, got {logits.device}")
+    if stream is not None:
+        with on_stream(index, stream, logits, targets, workspace) as there:
+            return there.returned(token_logprobs(logits, targets, n_top, workspace))
     code = _dtype_code(logits.dtype, "logits")
     if logits.dim() != 2:
         raise ValueError(f"logits must be [rows, vocab], got {tuple(logits.shape)}")
@@ -426,14 +429,12 @@ def token_logprobs(logits, targets=None, n_top: int = 0, workspace=None, stream=
         top_ids = torch.empty((rows, n_top), dtype=torch.int64, device=device)
         top_logprobs = torch.empty((rows, n_top), dtype=torch.float32, device=device)
         id_ptr, top_ptr = top_ids.data_ptr(), top_logprobs.data_ptr()
-    if stream is not None:
-        _used_on(stream, logprobs, entropy, top_ids, top_logprobs)
     if workspace is None:
-        workspace = _workspace(rrq_token_logprobs_workspace(rows, vocab, n_top), device, stream)
+        workspace = _workspace(rrq_token_logprobs_workspace(rows, vocab, n_top), device)
     w, w_bytes = _workspace_args(workspace, index)
     st = (_lib or _library()).rrq_token_logprobs(
         logits.data_ptr(), code, rows, vocab, row_stride if rows > 1 else vocab, target_ptr, n_top,
-        logprob_ptr, entropy.data_ptr(), id_ptr, top_ptr, w, w_bytes, _stream(stream))
+        logprob_ptr, entropy.data_ptr(), id_ptr, top_ptr, w, w_bytes, _stream(None))
     if st != RRQ_OK:
         raise RRQError(st, "rrq_token_logprobs")
     return logprobs, entropy, top_ids, top_logprobs
