@@ -1,4 +1,7 @@
-"""Where a tensor-level call works: on the stream it is given.
+"""Where a tensor-level call works: on the GPU of its tensors, and there on the
+stream it is given.
+
+A kernel launched while another GPU is the current one would run on that GPU.
 
 Memory that torch allocates belongs to the stream that was current then: it may
 still be read by work queued on that stream (a tensor freed a moment ago), so a
@@ -13,7 +16,10 @@ import torch
 
 
 def _stream_on(index: int, stream):
-    """The torch stream that a stream object or a raw handle names."""
+    """The torch stream that a stream object or a raw handle names; the current
+    one of that GPU for None."""
+    if stream is None:
+        return torch.cuda.current_stream(index)
     if not isinstance(stream, torch.cuda.Stream):
         handle = stream if isinstance(stream, int) else stream.cuda_stream
         if handle == 0:         # (an ExternalStream of 0 would be a stream of torch's pool)
@@ -24,8 +30,14 @@ def _stream_on(index: int, stream):
     return stream
 
 
+def elsewhere(index: int, stream) -> bool:
+    """Whether a call on cuda:index has to leave the caller's GPU or stream."""
+    return stream is not None or torch._C._cuda_getDevice() != index
+
+
 class on_stream:
-    """Context in which `stream` is the current one of cuda:index.
+    """Context in which cuda:index is the current GPU and `stream` its current
+    stream.
 
     `used` are the tensors of the call (others are passed over): once it is
     enqueued, none of them is handed out again before `stream` has passed it. What

@@ -18,9 +18,9 @@ descriptor of them; a program makes them once and updates the tensors in place
 (``lengths`` on the device from step to step).
 
 ``stream`` (a torch stream or a raw handle; by default torch's current stream) is
-where a call allocates and works. The caller orders it after the work that made
-the inputs, and orders the use of the outputs after it; the tensors themselves
-may be let go at once.
+where a call allocates and works, on the GPU of its tensors whichever is current.
+The caller orders it after the work that made the inputs, and orders the use of
+the outputs after it; the tensors themselves may be let go at once.
 """
 
 from __future__ import annotations
@@ -32,7 +32,7 @@ import torch
 
 from . import (RRQ_BF16, RRQ_F32, RRQ_OK, RRQError, _check_device_tensor, _ptr, _stream,
                load_library)
-from .placement import on_stream
+from .placement import elsewhere, on_stream
 
 RRQ_CODE_INT8 = 0
 RRQ_CODE_FP8 = 1
@@ -279,7 +279,7 @@ def cache_write(cache: KVCache, batch: CacheBatch, K, V, stream=None) -> None:
     bfloat16, any token and head strides of whole 16 bytes) into the batch's
     pages."""
     index = _device_index(cache, batch)
-    if stream is not None:
+    if elsewhere(index, stream):
         with on_stream(index, stream, *cache.tensors, *batch.tensors, K, V):
             return cache_write(cache, batch, K, V)
     rows, heads, dim = batch.n_tokens, cache.n_kv_heads, cache.head_dim
@@ -298,7 +298,7 @@ def cache_read(cache: KVCache, batch: CacheBatch, dtype=None, stream=None, out=N
     """(K, V) [n_tokens, n_kv_heads, head_dim] of the batch's tokens, dequantised
     to float32 or bfloat16 (the default). ``out`` may pass the pair."""
     index = _device_index(cache, batch)
-    if stream is not None:
+    if elsewhere(index, stream):
         used = (*cache.tensors, *batch.tensors, *(() if out is None else out))
         with on_stream(index, stream, *used) as there:
             return there.returned(cache_read(cache, batch, dtype, out=out))
@@ -358,7 +358,7 @@ def cache_attention(cache: KVCache, batch: CacheBatch, Q, scale=None, causal: bo
     over the batch's sequences: [n_tokens, n_heads, head_dim] in bfloat16 (the
     default) or float32. scale defaults to head_dim ** -0.5; window 0 is none."""
     index = _device_index(cache, batch)
-    if stream is not None:
+    if elsewhere(index, stream):
         with on_stream(index, stream, *cache.tensors, *batch.tensors, Q, workspace, out) as there:
             return there.returned(cache_attention(cache, batch, Q, scale, causal, window,
                                                   out_dtype, workspace, out=out))
@@ -404,7 +404,7 @@ def token_logprobs(logits, targets=None, n_top: int = 0, workspace=None, stream=
     index = logits.get_device()
     if index < 0:
         raise ValueError(f"logits must be on a GPU device, got {logits.device}")
-    if stream is not None:
+    if elsewhere(index, stream):
         with on_stream(index, stream, logits, targets, workspace) as there:
             return there.returned(token_logprobs(logits, targets, n_top, workspace))
     code = _dtype_code(logits.dtype, "logits")
