@@ -140,7 +140,7 @@ __device__ __forceinline__ bool split_tiles(const Attend &a, int lo, int hi, int
     return n == 1;
 }
 
-// What a range without keys leaves for the join: a sum of 0, no output. Grids
+// What a range without keys leaves for the join: a sum of 0, no mean. Grids
 // are as deep as the longest sequence may need, so most workgroups of a ragged
 // batch end here; they load no queries and pass no barrier.
 template <int R>
@@ -203,6 +203,15 @@ constexpr float kSumUnit = 0x1p-14f;
 __device__ __forceinline__ float scale_back(float vs, float vref)
 {
     return vs > 0.0f ? fminf(vref * kSumUnit * __builtin_amdgcn_rcpf(vs), 0x1p86f) : 0x1p46f;
+}
+
+// What turns a sum of weighted codes, in kSumUnit, into their mean value. At
+// most the scale of the largest contribution, as the sum counts that one with
+// vref / vs: a mean passes the largest value by its rounding at most, where
+// the sum times vref may pass binary32's range.
+__device__ __forceinline__ float mean_factor(float vref, float sum)
+{
+    return sum == 0.0f ? 0.0f : vref / sum;
 }
 
 // Queries go to binary16 times `up`, a power of two that brings the row's

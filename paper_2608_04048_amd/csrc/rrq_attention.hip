@@ -268,7 +268,8 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
     }
 
     // Join the waves, 16 rows at a time: lane (col, g) holds channels
-    // 16 n + 4 g + c of row col.
+    // 16 n + 4 g + c of row col. A wave leaves its own mean (mean_factor), and
+    // the means are joined by their shares of the sum.
 #pragma unroll
     for (int b = 0; b < NQ; ++b) {
         const float sum = group_sum(l[b]);
@@ -279,8 +280,10 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
                 lds_ml[(wave * rows_max + col) * 2 + 1] = sum;
             }
             float *dst = lds + (wave * rows_max + col) * (D + 4) + 4 * g;
+            const float norm = mean_factor(vref, sum);
 #pragma unroll
-            for (int n = 0; n < ND; ++n) *reinterpret_cast<f32x4 *>(dst + 16 * n) = o[b][n] * kSumUnit * vref;
+            for (int n = 0; n < ND; ++n)
+                *reinterpret_cast<f32x4 *>(dst + 16 * n) = o[b][n] * kSumUnit * norm;
         }
         __syncthreads();
         // 4 channels a thread
@@ -292,14 +295,19 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
 #pragma unroll
             for (int w = 0; w < NW; ++w) mm = fmaxf(mm, lds_ml[(w * rows_max + orow) * 2]);
             const float ms = mm == -kInf ? 0.0f : mm;
-            f32x4 y = {0, 0, 0, 0};
+            float f[NW];
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
                 const int at = w * rows_max + orow;
-                const float f = exp2_fast(lds_ml[at * 2] - ms);
-                ll += f * lds_ml[at * 2 + 1];
-                y += f * *reinterpret_cast<const f32x4 *>(lds + at * (D + 4) + d);
+                f[w] = exp2_fast(lds_ml[at * 2] - ms) * lds_ml[at * 2 + 1];
+                ll += f[w];
             }
+            const float norm = ll == 0.0f ? 0.0f : 1.0f / ll;
+            f32x4 y = {0, 0, 0, 0};
+#pragma unroll
+            for (int w = 0; w < NW; ++w)
+                y += f[w] * norm *
+                     *reinterpret_cast<const f32x4 *>(lds + (w * rows_max + orow) * (D + 4) + d);
             const RowPlace place = place_of(a, row0 + orow);
             const int64_t at = (int64_t)(r.o0 + place.token) * a.n_heads + kvh * a.ratio +
                                place.member;
@@ -313,7 +321,6 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
                 *reinterpret_cast<f32x4 *>(a.part_o + part * D + d) = y;
                 continue;
             }
-            y *= ll == 0.0f ? 0.0f : 1.0f / ll;
             if (a.out_bf16)
                 *reinterpret_cast<u32x2v *>(static_cast<uint16_t *>(a.out) + at * D + d) =
                     u32x2v{bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3])};
@@ -323,11 +330,11 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
     }
 }
 
-// Joins the key ranges of a row (token, head): W waves a row, wave w takes
-// ranges w, w + W, ..., 4 / W rows a workgroup. Lane s holds range s's maximum
-// and sum, so the factors cost one load. The ranges up to the last with a sum
-// were all written; they are read four at a time, those past it as the last,
-// times 0.
+// Joins the key ranges of a row (token, head), each of which left its mean, its
+// maximum and its sum: W waves a row, wave w takes ranges w, w + W, ..., 4 / W
+// rows a workgroup. Lane s holds range s's maximum and sum, so the factors cost
+// one load. The ranges up to the last with a sum were all written; they are read
+// four at a time, those past it as the last, times 0.
 template <int D, int W>
 __global__ __launch_bounds__(256) void attend_join_kernel(Attend a)
 {
@@ -346,10 +353,11 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Attend a)
     float m = ml[0];
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
-    const float f = exp2_fast(ml[0] - (m == -kInf ? 0.0f : m));
-    float l = f * ml[1];
+    float f = exp2_fast(ml[0] - (m == -kInf ? 0.0f : m)) * ml[1];
+    float l = f;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
+    f *= l == 0.0f ? 0.0f : 1.0f / l;
     const uint64_t has = __ballot(ml[1] != 0.0f);
     const int last = has ? 63 - __builtin_clzll(has) : -1;
     float y[N] = {};
@@ -379,15 +387,13 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Attend a)
 #pragma unroll
             for (int w = 1; w < W; ++w) y[d] += lds[w][lane * N + d];
     }
-    const float norm = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
     for (int d = 0; d < N; ++d) {
-        const float v = y[d] * norm;
         const int64_t i = at * D + lane * N + d;
         if (a.out_bf16)
-            static_cast<uint16_t *>(a.out)[i] = (uint16_t)bf16_bits(v);
+            static_cast<uint16_t *>(a.out)[i] = (uint16_t)bf16_bits(y[d]);
         else
-            static_cast<float *>(a.out)[i] = v;
+            static_cast<float *>(a.out)[i] = y[d];
     }
 }
 

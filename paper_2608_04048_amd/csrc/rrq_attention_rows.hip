@@ -367,6 +367,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
     l += __shfl_xor(l, 32);
     if (!live) return;
     const int64_t at = (r.o0 + token) * a.n_heads + head;
+    const float norm = mean_factor(vref, l);
     if (alone && a.n_splits > 1 && hb == 0) a.part_ml[2 * at + 1] = kAlone;
     if (!alone) {
         const int64_t part = (int64_t)blockIdx.y * a.batch.n_tokens * a.n_heads + at;
@@ -380,16 +381,16 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
 #pragma unroll
             for (int g = 0; g < 4; ++g)
                 *reinterpret_cast<f32x4 *>(dst + 32 * n + 8 * g) =
-                    f32x4{o[n][4 * g], o[n][4 * g + 1], o[n][4 * g + 2], o[n][4 * g + 3]} * kSumUnit * vref;
+                    f32x4{o[n][4 * g], o[n][4 * g + 1], o[n][4 * g + 2], o[n][4 * g + 3]} *
+                    kSumUnit * norm;
         return;
     }
-    const float norm = l == 0.0f ? 0.0f : vref * kSumUnit / l;
 #pragma unroll
     for (int n = 0; n < ND; ++n)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const f32x4 y = f32x4{o[n][4 * g], o[n][4 * g + 1], o[n][4 * g + 2],
-                                  o[n][4 * g + 3]} * norm;
+                                  o[n][4 * g + 3]} * kSumUnit * norm;
             const int64_t d = at * D + 32 * n + 8 * g + 4 * hb;
             if (a.out_bf16)
                 *reinterpret_cast<u32x2v *>(static_cast<uint16_t *>(a.out) + d) =
