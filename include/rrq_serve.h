@@ -162,14 +162,17 @@ int rrq_cache_read(const rrq_cache *cache, const rrq_batch *batch, void *K_out, 
  *              content is of no use before or after the call; calls that may
  *              run at the same time need their own.
  *
- * Arithmetic: queries are rounded to 11 significant bits (bfloat16 ones are
- * exact) relative to their row's largest, codes are exact, products are
- * summed in binary32; the softmax's sum is binary32; its weights, each with
- * its block's value scale, are rounded to 11 bits before the second product,
- * and those below 2^-20 of the row's largest to 2^-31 of it. (Value scales of
- * one sequence and head are taken to lie within a factor of 2^100 of each
- * other; smaller ones count as at that distance.) Results are deterministic for one shape of call; they may differ in the last bits
- * between calls of another batch.
+ * Arithmetic: codes are exact, products are summed in binary32, and so is the
+ * softmax's sum. The other operands are rounded according to the result. For
+ * bfloat16 (8 bits): queries to 11 significant bits relative to their row's
+ * largest (bfloat16 ones are exact), the softmax's weights, each with its block's
+ * value scale, to 11 bits before the second product, and those below 2^-20 of
+ * the row's largest to 2^-31 of it. For binary32 both go in as two parts of 11
+ * bits: 22 bits, and 2^-39 of the row's largest weight (at about twice the
+ * products' time, where those bound the call). (Value scales of one sequence and
+ * head are taken to lie within a factor of 2^100 of each other; smaller ones
+ * count as at that distance.) Results are deterministic for one shape of call;
+ * they may differ in the last bits between calls of another batch.
  *
  * Returns RRQ_OK, or RRQ_ERR_NULL / _ALIGN / _SHAPE / _DTYPE / _FORMAT /
  * _WORKSPACE with nothing enqueued, or RRQ_ERR_HIP.

@@ -67,9 +67,11 @@ constexpr unsigned few_lds(int D, int waves, int rows)
 // registers of a compute unit hold.
 constexpr int many_waves(int D) { return D == 64 ? 16 : 8; }
 
-// NW: waves; NQ: blocks of 16 rows of the row tile.
-template <int D, int CODE, int NW, int NQ>
-__global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_kernel(Attend a)
+// NW: waves; NQ: blocks of 16 rows of the row tile; PARTS: of an operand
+// (rrq_attention.h).
+template <int D, int CODE, int NW, int NQ, int PARTS>
+__global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 || PARTS > 1 ? 1 : 2)
+void attend_kernel(Attend a)
 {
     constexpr int KL = D / 64;      // 16-byte key loads a lane and key row
     constexpr int ND = D / 16;      // 16-channel tiles of the output
@@ -110,7 +112,7 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
     // This lane's rows, and their queries: lane (col, g) holds channels
     // 64 j + 16 g .. + 15.
     int lo[NQ], hi[NQ];
-    f16x8 q[NQ][KL][2];
+    f16x8 q[PARTS][NQ][KL][2];
     float qf[NQ];
 #pragma unroll
     for (int b = 0; b < NQ; ++b) {
@@ -134,7 +136,12 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) q[b][j][h][i] = (_Float16)(x[j][8 * h + i] * up);
+                for (int i = 0; i < 8; ++i) {
+                    const float y = x[j][8 * h + i] * up;
+                    q[0][b][j][h][i] = (_Float16)y;
+                    if (PARTS > 1)
+                        q[PARTS - 1][b][j][h][i] = (_Float16)(y - (float)q[0][b][j][h][i]);
+                }
     }
 
     float m[NQ], l[NQ], vref = 0.0f;
@@ -186,8 +193,10 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
                     const f16x8 k = codes_f16<CODE>(kw[i][j][2 * h], kw[i][j][2 * h + 1]);
 #pragma unroll
                     for (int b = 0; b < NQ; ++b)
-                        acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[b][j][h], acc[b], 0,
-                                                                        0, 0);
+#pragma unroll
+                        for (int t = 0; t < PARTS; ++t)
+                            acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[t][b][j][h],
+                                                                            acc[b], 0, 0, 0);
                 }
 #pragma unroll
             for (int b = 0; b < NQ; ++b)
@@ -229,7 +238,7 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
             vref = vmax;
         }
         const float back = scale_back(vs, vref), lback = __builtin_amdgcn_logf(back);
-        f16x8 p[NQ][2];
+        f16x8 p[PARTS][NQ][2];
         float alpha[NQ];
 #pragma unroll
         for (int b = 0; b < NQ; ++b) {
@@ -250,7 +259,10 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
                 for (int c = 0; c < 4; ++c) {
                     const float w = exp2_fast(s[b][i][c] - sub);
                     sum += w;       // (before it is rounded: it may be below binary16)
-                    p[b][i >> 1][4 * (i & 1) + c] = (_Float16)w;
+                    const _Float16 first = (_Float16)w;
+                    p[0][b][i >> 1][4 * (i & 1) + c] = first;
+                    if (PARTS > 1)
+                        p[PARTS - 1][b][i >> 1][4 * (i & 1) + c] = (_Float16)(w - (float)first);
                 }
             l[b] = l[b] * alpha[b] + sum * back;
         }
@@ -260,9 +272,13 @@ __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 ? 1 : 2) void attend_ke
             const f16x8 v1 = codes_f16<CODE>(vw[n][2], vw[n][3]);
 #pragma unroll
             for (int b = 0; b < NQ; ++b) {
-                o[b][n] *= alpha[b];
-                o[b][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[b][0], o[b][n], 0, 0, 0);
-                o[b][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[b][1], o[b][n], 0, 0, 0);
+                f32x4 y = o[b][n] * alpha[b];
+#pragma unroll
+                for (int t = 0; t < PARTS; ++t) {
+                    y = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[t][b][0], y, 0, 0, 0);
+                    y = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[t][b][1], y, 0, 0, 0);
+                }
+                o[b][n] = y;
             }
         }
     }
@@ -397,19 +413,29 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Attend a)
     }
 }
 
-template <int D, int CODE>
-hipError_t few_code(const Attend &a, const AttendPlan &p, hipStream_t stream)
+template <int D, int CODE, int PARTS>
+hipError_t few_parts(const Attend &a, const AttendPlan &p, hipStream_t stream)
 {
     const dim3 grid((unsigned)attend_row_tiles(a.batch, a.ratio, p.tile), a.cache.n_kv_heads,
                     a.n_splits);
-    const unsigned bytes = few_lds(D, p.waves, a.lds_rows);
+    // (two parts of heads of 256 pass the registers of a wave of eight)
+    constexpr int MANY = D == 256 && PARTS > 1 ? 4 : many_waves(D);
     if (p.waves > 4)
-        attend_kernel<D, CODE, many_waves(D), 1><<<grid, 64 * many_waves(D), bytes, stream>>>(a);
+        attend_kernel<D, CODE, MANY, 1, PARTS>
+            <<<grid, 64 * MANY, few_lds(D, MANY, a.lds_rows), stream>>>(a);
     else if (p.tile == kWideTile)
-        attend_kernel<D, CODE, 4, D <= 128 ? 2 : 1><<<grid, 256, bytes, stream>>>(a);
+        attend_kernel<D, CODE, 4, D <= 128 ? 2 : 1, PARTS>
+            <<<grid, 256, few_lds(D, 4, a.lds_rows), stream>>>(a);
     else
-        attend_kernel<D, CODE, 4, 1><<<grid, 256, bytes, stream>>>(a);
+        attend_kernel<D, CODE, 4, 1, PARTS>
+            <<<grid, 256, few_lds(D, 4, a.lds_rows), stream>>>(a);
     return hipGetLastError();
+}
+
+template <int D, int CODE>
+hipError_t few_code(const Attend &a, const AttendPlan &p, hipStream_t stream)
+{
+    return a.out_bf16 ? few_parts<D, CODE, 1>(a, p, stream) : few_parts<D, CODE, 2>(a, p, stream);
 }
 
 template <int D>

@@ -34,9 +34,10 @@
 namespace rrq_detail {
 namespace {
 
-constexpr float kSlack = 8.0f;
 // Weights carry a factor of 2^6: with the slack's 2^8 they reach 2^14 in
-// binary16, and its normal range ends at 2^-20 of a row's largest weight.
+// binary16, and its normal range ends at 2^-20 of a row's largest weight. Weights
+// of two parts need that range: no slack, 2^14.
+constexpr float slack(int parts) { return parts > 1 ? 0.0f : 8.0f; }
 
 // Passes a NaN on, unlike fmaxf, which needs its operands quieted first.
 __device__ __forceinline__ float maximum(float a, float b)
@@ -70,15 +71,17 @@ __device__ __forceinline__ int channel_of(int slot)
     return slot < KP ? 16 * slot : 16 * (slot - KP) + 8;
 }
 
-// KEYS: keys of a tile, 32 or 64.
-template <int D, int CODE, int KEYS>
-__global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
+// KEYS: keys of a tile, 32 or 64; PARTS: of an operand (rrq_attention.h), two of
+// which take the registers of a whole wave a SIMD.
+template <int D, int CODE, int KEYS, int PARTS>
+__global__ __launch_bounds__(256, PARTS > 1 ? 1 : 2) void attend_rows_kernel(Attend a)
 {
     constexpr int KROW = D * 2 + 16;        // LDS bytes of a key row: 16 more than a
     constexpr int VROW = KEYS * 2 + 16;    // multiple of 128, so 8 rows span all banks
     constexpr int KB = KEYS * KROW, VB = D * VROW;
     constexpr int BUF = KB + VB + 64;       // and the scales of its runs
     constexpr int R = kRowsTile;
+    constexpr float kSlack = slack(PARTS);
     constexpr int KT = KEYS * D / 16 / 256;    // 16-code pieces a thread stages
     constexpr int ND = D / 32, NK = D / 16, NH = KEYS / 32, RUNS = KEYS / 16;
     __shared__ __attribute__((aligned(16))) uint8_t lds[2 * BUF];
@@ -115,7 +118,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
 
     // queries: lane (col, hb) holds 8 channels of its row a product, in the
     // order in which key rows stand in LDS
-    f16x8 q[NK];
+    f16x8 q[PARTS][NK];
     float qf;
     {
         float x[NK][8];
@@ -133,7 +136,11 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
 #pragma unroll
         for (int j = 0; j < NK; ++j)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) q[j][e] = (_Float16)(x[j][e] * up);
+            for (int e = 0; e < 8; ++e) {
+                const float y = x[j][e] * up;
+                q[0][j][e] = (_Float16)y;
+                if (PARTS > 1) q[PARTS - 1][j][e] = (_Float16)(y - (float)q[0][j][e]);
+            }
     }
 
     // Staging. Keys: thread t takes 16-code piece t % KP of key rows t / KP +
@@ -283,7 +290,9 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
             for (int h = 0; h < NH; ++h) {
                 const f16x8 k =
                     *reinterpret_cast<const f16x8 *>(krows + 32 * h * KROW + 32 * j);
-                s[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[j], s[h], 0, 0, 0);
+#pragma unroll
+                for (int t = 0; t < PARTS; ++t)
+                    s[h] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[t][j], s[h], 0, 0, 0);
             }
         }
         store_tile(lds + ((tile + 1) & 1) * BUF);
@@ -333,8 +342,8 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
 #pragma unroll
             for (int n = 0; n < ND; ++n) o[n] *= alpha;
         }
-        const float ms = (m == -kInf ? 0.0f : m) - 6.0f;    // - 6: the weights' factor
-        f16x8 p[RUNS];
+        const float ms = (m == -kInf ? 0.0f : m) - (14.0f - kSlack);    // the weights' factor
+        f16x8 p[PARTS][RUNS];
 #pragma unroll
         for (int i = 0; i < RUNS; ++i) {
             const float sub = ms + lane_value(lbacks, i);
@@ -345,7 +354,8 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
             for (int e = 0; e < 8; ++e) {
                 const float w = exp2_fast(
                     __builtin_fmaf(s[i >> 1][8 * (i & 1) + e], c[i], -sub));
-                p[i][e] = (_Float16)w;
+                p[0][i][e] = (_Float16)w;
+                if (PARTS > 1) p[PARTS - 1][i][e] = (_Float16)(w - (float)p[0][i][e]);
                 sum += w;
             }
             l += sum * lane_value(backs, i);
@@ -358,7 +368,9 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
             for (int n = 0; n < ND; ++n) {
                 const f16x8 v =
                     *reinterpret_cast<const f16x8 *>(vrows + 32 * n * VROW + 32 * i);
-                o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[i], o[n], 0, 0, 0);
+#pragma unroll
+                for (int t = 0; t < PARTS; ++t)
+                    o[n] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, p[t][i], o[n], 0, 0, 0);
             }
         barrier();
     }
@@ -400,16 +412,24 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend a)
         }
 }
 
-template <int D>
-hipError_t rows_dim(const Attend &a, hipStream_t stream)
+template <int D, int CODE>
+hipError_t rows_code(const Attend &a, hipStream_t stream)
 {
     const dim3 grid((unsigned)(attend_row_tiles(a.batch, a.ratio, kRowsTile) *
                                a.cache.n_kv_heads), a.n_splits);
     constexpr int KEYS = D == 256 ? 32 : 64;
-    auto kernel = a.cache.code_type == RRQ_CODE_INT8 ? attend_rows_kernel<D, RRQ_CODE_INT8, KEYS>
-                                                     : attend_rows_kernel<D, RRQ_CODE_FP8, KEYS>;
-    kernel<<<grid, 256, 0, stream>>>(a);
+    if (a.out_bf16)
+        attend_rows_kernel<D, CODE, KEYS, 1><<<grid, 256, 0, stream>>>(a);
+    else
+        attend_rows_kernel<D, CODE, KEYS, 2><<<grid, 256, 0, stream>>>(a);
     return hipGetLastError();
+}
+
+template <int D>
+hipError_t rows_dim(const Attend &a, hipStream_t stream)
+{
+    return a.cache.code_type == RRQ_CODE_INT8 ? rows_code<D, RRQ_CODE_INT8>(a, stream)
+                                              : rows_code<D, RRQ_CODE_FP8>(a, stream);
 }
 
 }  // namespace

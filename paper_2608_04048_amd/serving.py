@@ -356,7 +356,9 @@ def cache_attention(cache: KVCache, batch: CacheBatch, Q, scale=None, causal: bo
                     window: int = 0, out_dtype=None, workspace=None, stream=None, out=None):
     """Attention of queries [n_tokens, n_heads, head_dim] (float32 or bfloat16)
     over the batch's sequences: [n_tokens, n_heads, head_dim] in bfloat16 (the
-    default) or float32. scale defaults to head_dim ** -0.5; window 0 is none."""
+    default) or float32. scale defaults to head_dim ** -0.5; window 0 is none. A
+    float32 result is computed with operands of 22 bits, a bfloat16 one of 11
+    (see rrq_serve.h)."""
     index = _device_index(cache, batch)
     if elsewhere(index, stream):
         with on_stream(index, stream, *cache.tensors, *batch.tensors, Q, workspace, out) as there:
