@@ -40,6 +40,9 @@ enum rrq_code_type {
  *   v_codes   device, [n_pages][n_kv_heads][head_dim][page_size], 16-byte aligned
  *             (both products of attention then read runs of bytes).
  *   k_scales, v_scales  device, float [n_pages][n_kv_heads], 4-byte aligned.
+ *             Scales of pages in use are finite and 0 or more, as rrq_cache_write
+ *             leaves them; with others, what is read from or attended over
+ *             their page and head is unspecified.
  *   n_pages   >= 1.
  *   n_kv_heads 1..1024.
  *   head_dim  64, 128 or 256.
@@ -156,7 +159,8 @@ int rrq_cache_read(const rrq_cache *cache, const rrq_batch *batch, void *K_out, 
  *   window     0 (none) or the number of positions a token sees, its own the
  *              last.
  *   out        device, out_dtype [n_tokens][n_heads][head_dim] contiguous,
- *              16-byte aligned (written): rows of rrq_linear's X.
+ *              16-byte aligned (written): rows of rrq_linear's X. Rows outside
+ *              offsets[0]..offsets[n_seqs]-1 are not written.
  *   workspace  device, 16-byte aligned, workspace_bytes of at least
  *              rrq_cache_attention_workspace's value (NULL if that is 0). Its
  *              content is of no use before or after the call; calls that may

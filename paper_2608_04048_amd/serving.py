@@ -151,8 +151,8 @@ def rrq_token_logprobs_workspace(n_rows: int, vocab: int, n_top: int) -> int:
 class KVCache:
     """One layer's 8-bit cache: k_codes uint8 [n_pages, n_kv_heads, page_size,
     head_dim], v_codes uint8 [n_pages, n_kv_heads, head_dim, page_size],
-    k_scales and v_scales float32 [n_pages, n_kv_heads], all contiguous on one
-    GPU. code_type: "int8" or "fp8" (e4m3)."""
+    k_scales and v_scales float32 [n_pages, n_kv_heads] (finite, 0 or more), all
+    contiguous on one GPU. code_type: "int8" or "fp8" (e4m3)."""
 
     def __init__(self, k_codes, v_codes, k_scales, v_scales, code_type: str = "int8"):
         if code_type not in CODE_TYPES:
