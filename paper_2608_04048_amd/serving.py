@@ -17,6 +17,9 @@ A ``KVCache`` and a ``CacheBatch`` keep the tensors they were made of and a C
 descriptor of them; a program makes them once and updates the tensors in place
 (``lengths`` on the device from step to step).
 
+Forward only: no call records a graph for gradients, and results of inputs that
+require one are detached.
+
 ``stream`` (a torch stream or a raw handle; by default torch's current stream) is
 where a call allocates and works, on the GPU of its tensors whichever is current.
 The caller orders it after the work that made the inputs, and orders the use of
