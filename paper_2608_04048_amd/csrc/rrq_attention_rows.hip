@@ -18,14 +18,16 @@
 // scale back once a run: l += (vref / vs) sum w. vref is a scale of the range
 // at hand that keeps the exponents small.
 //
-// Measured (8 kv heads of 128, int8): 4096 rows of 40 query heads on 16384
-// positions, 1.20 TFLOP in 1.33 ms, 905 TFLOP/s where a large binary16 product
-// of the library makes 1133; the matrix cores are busy 41% of the cycles. A wave
-// waits for its LDS operands and the softmax between its two products; two
-// workgroups a compute unit (LDS and registers hold no more) overlap. Five
-// chunks of 174 to 900 tokens, heads of 256, window 1024: 44 GFLOP in 106 us (420
-// TFLOP/s): 340 row tiles on 256 compute units, and 32-key tiles, as LDS holds
-// two workgroups' 64-key tiles of such heads no more (one a compute unit: 156 us).
+// Measured. 8 kv heads of 128, int8: 4096 rows of 40 query heads on 16384
+// positions, 1.20 TFLOP in 1.31 to 1.37 ms, 880 to 919 TFLOP/s where a large
+// binary16 product of the library makes 1133; the matrix cores are busy 40% of
+// the cycles. A wave waits for its LDS operands and the softmax between its two
+// products; two workgroups a compute unit (LDS and registers hold no more)
+// overlap. 4 kv heads of 256, e4m3: five chunks of 174 to 900 tokens, window 1024,
+// 44 GFLOP in 105 us (420 TFLOP/s): 340 row tiles on 256 compute units, and 32-key
+// tiles, as LDS holds two workgroups' 64-key tiles of such heads no more (one a
+// compute unit: 156 us). Registers are full there: 6 (int8) and 3 (e4m3) vector
+// registers spill, and 37 scalar ones with heads of 64.
 //
 // The running maximum m moves only when a tile's exceeds it by 8 (weights
 // then grow to 2^8 at most): most tiles skip the output's rescaling.
@@ -76,8 +78,9 @@ __device__ __forceinline__ int channel_of(int slot)
 template <int D, int CODE, int KEYS, int PARTS>
 __global__ __launch_bounds__(256, PARTS > 1 ? 1 : 2) void attend_rows_kernel(Attend a)
 {
-    constexpr int KROW = D * 2 + 16;        // LDS bytes of a key row: 16 more than a
-    constexpr int VROW = KEYS * 2 + 16;    // multiple of 128, so 8 rows span all banks
+    // LDS bytes of a row. 16 more than a multiple of 128, so that 8 rows span all
+    // banks (values of 32-key tiles: 80, an odd number of 16s, which does as well).
+    constexpr int KROW = D * 2 + 16, VROW = KEYS * 2 + 16;
     constexpr int KB = KEYS * KROW, VB = D * VROW;
     constexpr int BUF = KB + VB + 64;       // and the scales of its runs
     constexpr int R = kRowsTile;
