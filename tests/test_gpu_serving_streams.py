@@ -118,3 +118,33 @@ def test_an_error_leaves_the_current_stream(gpu):
     with pytest.raises(gpu.RRQError):
         gpu.token_logprobs(torch.zeros((2, 40), device="cuda"), n_top=33, stream=side)
     assert torch.cuda.current_stream() == before
+
+
+def test_a_captured_call_that_names_its_stream(gpu):
+    """Inputs from the default stream, captured on a stream given by name;
+    replayed on new inputs, with eager calls between."""
+    import torch
+    s, _ = _calls(gpu)
+    Q = torch.randn((1000, 8, 128), device="cuda")
+    logits = torch.randn((1000, 20000), device="cuda")
+    side = torch.cuda.Stream()
+
+    def step(**kw):
+        return (gpu.cache_attention(s.cache, s.batch, Q, **kw),
+                *gpu.cache_read(s.cache, s.batch, **kw),
+                *gpu.token_logprobs(logits, None, 3, **kw)[1:])
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        captured = step(stream=side)
+    for seed in range(4):
+        Q.normal_()
+        logits.normal_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in captured]
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), seed
