@@ -1,0 +1,90 @@
+"""Plain CPU definitions of the calls of include/rrq_draft.h, written from the
+header's formulas in numpy, in 64 bits.
+"""
+
+import numpy as np
+
+U = 2.0 ** -24          # half a step of binary32, relative
+
+
+def normed(x, kind, eps):
+    """Rows of x normed, without weights."""
+    if kind == "layer":
+        x = x - x.mean(1, keepdims=True)
+    with np.errstate(invalid="ignore", divide="ignore"):
+        return x / np.sqrt(np.square(x).mean(1, keepdims=True) + eps)
+
+
+def block_norm(residual, y, weight, bias, kind, post, post_weight, gate, scale, eps):
+    """(out, h) in 64 bits."""
+    h = residual.astype(np.float64)
+    if y is not None:
+        y = y.astype(np.float64)
+        if post:
+            y = normed(y, post, eps)
+            if post_weight is not None:
+                y = y * post_weight.astype(np.float64)
+        if gate is not None:
+            y = gate.astype(np.float64) * y
+        h = h + scale * y
+    out = normed(h, kind, eps)
+    if weight is not None:
+        out = out * weight.astype(np.float64)
+    return (out if bias is None else out + bias.astype(np.float64)), h
+
+
+def _normed_error(x, dx, kind, eps, terms):
+    """How far a norm computed in binary32 may be off, for elements off by dx: sums
+    round `terms` times at most, each rounding is off by U of its result."""
+    if kind == "layer":
+        dm = dx.mean(1, keepdims=True) + terms * U * np.abs(x).mean(1, keepdims=True)
+        x = x - x.mean(1, keepdims=True)
+        dx = dx + dm + U * np.abs(x)
+    s = np.square(x).mean(1, keepdims=True) + eps
+    # 2 |x| dx + dx^2 a term
+    ds = (2 * np.abs(x) * dx + dx * dx).mean(1, keepdims=True) + terms * U * s
+    with np.errstate(invalid="ignore", divide="ignore"):
+        f = 1 / np.sqrt(s)
+        # 1 / sqrt(s - ds) - 1 / sqrt(s) bounds both sides; the square root, the
+        # quotient and the product with it round
+        worst = np.where(ds < s, 1 / np.sqrt(np.maximum(s - ds, 1e-300)), np.inf)
+        return dx * worst + np.abs(x) * ((worst - f) + 5 * U * f)
+
+
+def block_norm_error(residual, y, weight, bias, kind, post, post_weight, gate, scale, eps):
+    """(out, h): bounds of the binary32 arithmetic's errors, before results are
+    rounded to their types."""
+    # a thread's elements one after another (64 at most), lanes, waves; 1 / n, the
+    # product with it, and eps
+    terms = 64 + 6 + 16 + 3
+    h = residual.astype(np.float64)
+    dh = np.zeros_like(h)
+    if y is not None:
+        y = y.astype(np.float64)
+        dy = np.zeros_like(y)
+        if post:
+            dy = _normed_error(y, dy, post, eps, terms)
+            y = normed(y, post, eps)
+            if post_weight is not None:
+                w = post_weight.astype(np.float64)
+                y, dy = y * w, dy * np.abs(w)
+                dy = dy + U * np.abs(y)
+        if gate is not None:
+            g = gate.astype(np.float64)
+            y, dy = y * g, dy * np.abs(g)
+            dy = dy + U * np.abs(y)
+        y, dy = scale * y, abs(scale) * dy
+        dy = dy + U * np.abs(y)
+        h = h + y
+        dh = dy + U * np.abs(h)
+    d = _normed_error(h, dh, kind, eps, terms)
+    out = normed(h, kind, eps)
+    if weight is not None:
+        w = weight.astype(np.float64)
+        out, d = out * w, d * np.abs(w)
+        d = d + U * np.abs(out)
+    if bias is not None:
+        out = out + bias
+        d = d + U * np.abs(out)
+    # (products of two errors, and what binary32 loses below its range)
+    return d * 1.01 + 1e-37, dh * 1.01 + 1e-37

@@ -9,8 +9,9 @@ arguments: tensors become device pointers,
 the stream defaults to torch's current stream, and a nonzero status raises
 ``RRQError``. ``construct``, ``construct_from_base``, ``reconstruct`` and
 ``linear`` additionally allocate the output tensors with torch. ``serving`` binds
-include/rrq_serve.h (the 8-bit cache, attention over it, token scoring); its names
-are available here too. Every computation runs in the HIP kernels; there is
+include/rrq_serve.h (the 8-bit cache, attention over it, token scoring) and
+``drafting`` include/rrq_draft.h (the step of a decoder that drafts tokens); their
+names are available here too. Every computation runs in the HIP kernels; there is
 no fallback, and a missing library raises.
 """
 
@@ -404,13 +405,16 @@ def group_pmr(W, group_size: int = 128, stream=None):
     return out
 
 
-# serving needs torch at import; its names are loaded with their first use
+# serving and drafting need torch at import; their names are loaded with their first use
 _SERVING = frozenset((
     "CODE_TYPES", "RRQ_CODE_FP8", "RRQ_CODE_INT8", "RRQ_MAX_TOP", "CacheBatch", "KVCache",
     "RrqBatch", "RrqCache", "attention_workspace", "cache_attention", "cache_read", "cache_write",
     "logprobs_workspace", "rrq_cache_attention", "rrq_cache_attention_workspace",
     "rrq_cache_read", "rrq_cache_write", "rrq_token_logprobs", "rrq_token_logprobs_workspace",
     "token_logprobs"))
+_DRAFTING = frozenset((
+    "NORM_KINDS", "RRQ_NORM_LAYER", "RRQ_NORM_NONE", "RRQ_NORM_RMS", "RrqNorm", "block_norm",
+    "rrq_block_norm"))
 
 
 def __getattr__(name):
@@ -418,5 +422,10 @@ def __getattr__(name):
         from . import serving
         for n in _SERVING:
             globals()[n] = getattr(serving, n)
+        return globals()[name]
+    if name in _DRAFTING:
+        from . import drafting
+        for n in _DRAFTING:
+            globals()[n] = getattr(drafting, n)
         return globals()[name]
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -73,7 +73,7 @@ def build(keep_asm: bool = False) -> str:
     kern_objs, cmds = [], []
     for name in ("rrq_kernels", "rrq_linear", "rrq_decode", "rrq_batch", "rrq_prefill",
                  "rrq_split", "rrq_cache", "rrq_attention",
-                 "rrq_attention_rows", "rrq_logprobs"):
+                 "rrq_attention_rows", "rrq_logprobs", "rrq_norm"):
         obj = os.path.join(BUILD_DIR, name + ".o")
         cmd = [cc, *DEVICE_FLAGS, *SOURCE_FLAGS.get(name, []), f"-I{INCLUDE}", f"-I{CSRC}", "-c",
                os.path.join(CSRC, name + ".hip"), "-o", obj]
@@ -84,7 +84,7 @@ def build(keep_asm: bool = False) -> str:
     with ThreadPoolExecutor(max_workers=len(cmds)) as pool:
         list(pool.map(_run, cmds))
     api_objs = []
-    for name in ("rrq_api", "rrq_serve_api"):
+    for name in ("rrq_api", "rrq_serve_api", "rrq_draft_api"):
         obj = os.path.join(BUILD_DIR, name + ".o")
         _run([cc, "-x", "c++", *HOST_FLAGS, "-D__HIP_PLATFORM_AMD__", f"-I{INCLUDE}", f"-I{CSRC}",
               f"-I{ROCM}/include",

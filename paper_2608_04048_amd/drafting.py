@@ -1,0 +1,183 @@
+"""What a decoder that drafts tokens with a short prefix of its packages and
+checks them with a longer one runs beside the calls of ``serving``.
+
+Binding of include/rrq_draft.h in librrq.so. ``rrq_block_norm`` marshals
+arguments one to one; ``block_norm`` takes torch tensors, checks them and
+allocates the outputs. Every computation runs in the HIP kernels.
+
+    x, h = block_norm(h, y, weight)          # residual, and rrq_linear's next X
+
+Forward only, and ``stream`` as in ``serving``.
+"""
+
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+from . import RRQ_BF16, RRQ_F32, RRQ_OK, RRQError, _ptr, _stream, load_library
+from .placement import elsewhere, on_stream
+from .serving import _checked, _dtype_code
+
+RRQ_NORM_NONE = 0
+RRQ_NORM_RMS = 1
+RRQ_NORM_LAYER = 2
+NORM_KINDS = {"rms": RRQ_NORM_RMS, "layer": RRQ_NORM_LAYER}
+
+
+class RrqNorm(ctypes.Structure):
+    """struct rrq_norm of rrq_draft.h."""
+    _fields_ = [("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("post_weight", ctypes.c_void_p), ("kind", ctypes.c_int32),
+                ("post", ctypes.c_int32), ("eps", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
+_lib = None
+
+
+def _library():
+    global _lib
+    if _lib is None:
+        lib = load_library()
+        P, I64, I32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32
+        for name, args in (
+                ("rrq_block_norm", [P, P, I32, I64, P, I32, I64, P, I64, I64, I64, P, I32, P, P]),):
+            f = getattr(lib, name)
+            f.argtypes, f.restype = args, ctypes.c_int
+        _lib = lib
+    return _lib
+
+
+# ---------------------------------------------------------------------------
+# C ABI, one to one (norm: RrqNorm)
+# ---------------------------------------------------------------------------
+
+def rrq_block_norm(norm, residual, residual_dtype: int, residual_stride: int, y, y_dtype: int,
+                   y_stride: int, gate, gate_stride: int, n_rows: int, hidden: int, out,
+                   out_dtype: int, h, stream=None) -> None:
+    """Enqueue the norms between two blocks (see rrq_draft.h)."""
+    _checked(_library().rrq_block_norm(ctypes.byref(norm), _ptr(residual), residual_dtype,
+                                       residual_stride, _ptr(y), y_dtype, y_stride, _ptr(gate),
+                                       gate_stride, n_rows, hidden, _ptr(out), out_dtype, _ptr(h),
+                                       _stream(stream)), "rrq_block_norm")
+
+
+# ---------------------------------------------------------------------------
+# Tensor-level helpers
+# ---------------------------------------------------------------------------
+
+def _matrix(t, name: str, rows: int, cols: int, index: int) -> int:
+    """Checks that t is [rows, cols] on the GPU of that index, contiguous in its
+    last dimension; its row stride."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.get_device() != index:
+        raise ValueError(f"{name} must be on cuda:{index}, got {t.device}")
+    if tuple(t.shape) != (rows, cols):
+        raise ValueError(f"{name} must be {(rows, cols)}, got {tuple(t.shape)}")
+    stride, one = t.stride()
+    if one != 1 and cols > 1:
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+    return stride
+
+
+def _vector(t, name: str, cols: int, dtype, index: int):
+    """Address of a contiguous vector; None for None."""
+    if t is None:
+        return None
+    if (not isinstance(t, torch.Tensor) or t.dtype != dtype or t.get_device() != index or
+            tuple(t.shape) != (cols,) or not t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor [{cols}] on cuda:{index}")
+    return t.data_ptr()
+
+
+def block_norm(residual, y=None, weight=None, bias=None, kind: str = "rms", post=None,
+               post_weight=None, gate=None, scale: float = 1.0, eps: float = 1e-6, out_dtype=None,
+               stream=None, out=None):
+    """(out, h) of h = residual + scale * gate * post(y) * post_weight and
+    out = kind(h) * weight + bias, row by row.
+
+    residual [rows, hidden] and the block's output y of that shape are float32 or
+    bfloat16 each, their rows may be strided (columns of a wider tensor); without y
+    the residual is normalised and returned as h. kind is "rms" or "layer", post
+    one of them or None (no norm of y). weight, bias and post_weight are float32
+    [hidden] or None. gate, of y's type, is [hidden] or [rows, hidden] (rows may be
+    strided). h has the residual's type, out is bfloat16 (the default: rrq_linear's
+    X) or float32. ``out`` may pass the pair; its second may be the residual
+    itself, which is then updated in place."""
+    if not isinstance(residual, torch.Tensor):
+        raise TypeError("residual must be a torch.Tensor")
+    index = residual.get_device()
+    if index < 0:
+        raise ValueError(f"residual must be on a GPU device, got {residual.device}")
+    if elsewhere(index, stream):
+        used = (residual, y, weight, bias, post_weight, gate, *(() if out is None else out))
+        with on_stream(index, stream, *used) as there:
+            return there.returned(block_norm(residual, y, weight, bias, kind, post, post_weight,
+                                             gate, scale, eps, out_dtype, out=out))
+    kind_code = NORM_KINDS.get(kind)
+    post_code = RRQ_NORM_NONE if post is None else NORM_KINDS.get(post)
+    if kind_code is None or post_code is None:
+        raise ValueError(f"kind and post must be of {sorted(NORM_KINDS)} (post may be None), got "
+                         f"{kind!r} and {post!r}")
+    if residual.dim() != 2:
+        raise ValueError(f"residual must be [rows, hidden], got {tuple(residual.shape)}")
+    rows, cols = residual.shape
+    r_code = _dtype_code(residual.dtype, "residual")
+    r_stride = _matrix(residual, "residual", rows, cols, index)
+    y_ptr = gate_ptr = h_ptr = None
+    y_stride = gate_stride = 0
+    y_code = r_code
+    if y is None:
+        if post is not None or post_weight is not None or gate is not None:
+            raise ValueError("post, post_weight and gate need y")
+    else:
+        y_stride = _matrix(y, "y", rows, cols, index)
+        y_code = _dtype_code(y.dtype, "y")
+        y_ptr = y.data_ptr()
+        if post is None and post_weight is not None:
+            raise ValueError("post_weight needs post")
+        if gate is not None:
+            if isinstance(gate, torch.Tensor) and gate.dim() == 2:
+                gate_stride = _matrix(gate, "gate", rows, cols, index)
+                if gate.dtype != y.dtype:
+                    raise TypeError(f"gate must have y's dtype {y.dtype}, got {gate.dtype}")
+                gate_ptr = gate.data_ptr()
+                if rows > 1 and gate_stride < cols:
+                    raise ValueError("gate's rows must not overlap; one row for all is [hidden]")
+            else:
+                gate_ptr = _vector(gate, "gate", cols, y.dtype, index)
+    if out is None:
+        out_dtype = torch.bfloat16 if out_dtype is None else out_dtype
+        out_code = _dtype_code(out_dtype, "out_dtype")
+        x = torch.empty((rows, cols), dtype=out_dtype, device=residual.device)
+        h = residual if y is None else torch.empty((rows, cols), dtype=residual.dtype,
+                                                   device=residual.device)
+    else:
+        x, h = out
+        for t, name in ((x, "out[0]"), (h, "out[1]")):
+            _matrix(t, name, rows, cols, index)
+            if not t.is_contiguous() and y is not None:
+                raise ValueError(f"{name} must be contiguous")
+        if not x.is_contiguous():
+            raise ValueError("out[0] must be contiguous")
+        out_code = _dtype_code(x.dtype, "out[0]")
+        if out_dtype is not None and x.dtype != out_dtype:
+            raise TypeError(f"out[0] must have dtype {out_dtype}, got {x.dtype}")
+        if h.dtype != residual.dtype:
+            raise TypeError(f"out[1] must have the residual's dtype, got {h.dtype}")
+        if y is None and h is not residual:
+            raise ValueError("without y, out[1] must be the residual itself")
+    if y is not None:
+        h_ptr = h.data_ptr()
+    norm = RrqNorm(_vector(weight, "weight", cols, torch.float32, index),
+                   _vector(bias, "bias", cols, torch.float32, index),
+                   _vector(post_weight, "post_weight", cols, torch.float32, index),
+                   kind_code, post_code, eps, scale)
+    st = (_lib or _library()).rrq_block_norm(
+        ctypes.byref(norm), residual.data_ptr(), r_code, r_stride, y_ptr, y_code, y_stride,
+        gate_ptr, gate_stride, rows, cols, x.data_ptr(), out_code, h_ptr, _stream(None))
+    if st != RRQ_OK:
+        raise RRQError(st, "rrq_block_norm")
+    return x, h
