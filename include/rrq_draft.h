@@ -77,6 +77,61 @@ int rrq_block_norm(const rrq_norm *norm, const void *residual, int32_t residual_
                    const void *gate, int64_t gate_stride, int64_t n_rows, int64_t hidden,
                    void *out, int32_t out_dtype, void *h, hipStream_t stream);
 
+/* Which channels a pair i of a rotation of rot_dim channels consists of. */
+enum rrq_rotary_layout {
+    RRQ_ROTARY_HALF = 0,            /* i and i + rot_dim / 2 */
+    RRQ_ROTARY_INTERLEAVED = 1      /* 2 i and 2 i + 1 */
+};
+
+/*
+ * rrq_rotary - rotary positions (host memory, read during the call).
+ *
+ *   frequencies  device, double [rot_dim / 2], 8-byte aligned: pair i of a token at
+ *                position p turns by the angle p frequencies[i] (radians). Any
+ *                schedule for long contexts is a choice of frequencies.
+ *   amplitude    factor of cosines and sines; finite.
+ *   rot_dim      the first rot_dim channels of a head are rotated, a multiple of 8,
+ *                8..head_dim; the others stay.
+ *   layout       enum rrq_rotary_layout.
+ */
+typedef struct rrq_rotary {
+    const double *frequencies;
+    double amplitude;
+    int32_t rot_dim;
+    int32_t layout;
+} rrq_rotary;
+
+/*
+ * rrq_cache_append - rotate the batch's queries and keys to their positions, and
+ * quantise keys and values into their pages.
+ *
+ *   positions  device, int32 [n_tokens], 4-byte aligned: the position each row is
+ *              rotated to (drafted tokens of a tree: by their depth), of any sign.
+ *              NULL: the row's place in its sequence.
+ *   Q          device, dtype (RRQ_F32 or RRQ_BF16) [n_tokens][n_heads][head_dim], K
+ *              and V as for rrq_cache_write, of the same dtype: columns of one
+ *              fused projection, with strides in elements; 16-byte aligned, strides
+ *              multiples of 16 bytes.
+ *   n_heads    query heads, 1..2^16 (any number).
+ *   Q_out      device, dtype [n_tokens][n_heads][head_dim] contiguous, 16-byte
+ *              aligned (written): the queries rotated. May be Q itself, where that is
+ *              contiguous. Rows outside offsets[0]..offsets[n_seqs]-1 are not written.
+ *
+ * With c = fl(amplitude cos t), s = fl(amplitude sin t) of the angle t in 64 bits,
+ * fl() one binary32 rounding, a pair (x, y) becomes
+ *   fl(fl(x c) - fl(y s)), fl(fl(y c) + fl(x s)),
+ * rounded to dtype in Q_out; keys go on in binary32, and keys and values are written
+ * as rrq_cache_write does. Angles up to 2^50 (NaN beyond or for frequencies that are
+ * not finite: unspecified codes, as for keys that are not finite).
+ *
+ * Returns as rrq_cache_write (_FORMAT for an unknown layout as well).
+ */
+int rrq_cache_append(const rrq_cache *cache, const rrq_batch *batch, const rrq_rotary *rotary,
+                     const int32_t *positions, const void *Q, const void *K, const void *V,
+                     int32_t dtype, int64_t q_token_stride, int64_t q_head_stride,
+                     int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
+                     int64_t v_head_stride, int32_t n_heads, void *Q_out, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -4,6 +4,9 @@ header's formulas in numpy, in 64 bits.
 
 import numpy as np
 
+from oracle import serving
+
+F32 = np.float32
 U = 2.0 ** -24          # half a step of binary32, relative
 
 
@@ -88,3 +91,34 @@ def block_norm_error(residual, y, weight, bias, kind, post, post_weight, gate, s
         d = d + U * np.abs(out)
     # (products of two errors, and what binary32 loses below its range)
     return d * 1.01 + 1e-37, dh * 1.01 + 1e-37
+
+
+def rotate(x, positions, frequencies, layout, amplitude):
+    """Rows x [tokens, heads, dim] (binary32) rotated, each operation rounded to
+    binary32; cosines and sines are rounded once."""
+    rot = 2 * len(frequencies)
+    angle = np.asarray(positions, np.float64)[:, None] * frequencies
+    c, s = ((amplitude * f(angle)).astype(F32)[:, None] for f in (np.cos, np.sin))
+    x = np.asarray(x, F32)
+    pick = ((slice(0, rot // 2), slice(rot // 2, rot)) if layout == "half" else
+            (slice(0, rot, 2), slice(1, rot, 2)))
+    a, b = x[..., pick[0]], x[..., pick[1]]
+    out = x.copy()
+    out[..., pick[0]] = a * c - b * s
+    out[..., pick[1]] = b * c + a * s
+    return out
+
+
+def places(lengths, offsets):
+    """Each row's place in its sequence."""
+    return [length - (offsets[b + 1] - offsets[b]) + i for b, length in enumerate(lengths)
+            for i in range(offsets[b + 1] - offsets[b])]
+
+
+def append(cache, table, lengths, offsets, positions, frequencies, layout, amplitude, Q, K, V):
+    """The rotated queries (binary32); keys and values are written in place."""
+    if positions is None:
+        positions = places(lengths, offsets)
+    turn = (positions, frequencies, layout, amplitude)
+    serving.write(cache, table, lengths, offsets, rotate(K, *turn), V)
+    return rotate(Q, *turn)

@@ -413,8 +413,9 @@ _SERVING = frozenset((
     "rrq_cache_read", "rrq_cache_write", "rrq_token_logprobs", "rrq_token_logprobs_workspace",
     "token_logprobs"))
 _DRAFTING = frozenset((
-    "NORM_KINDS", "RRQ_NORM_LAYER", "RRQ_NORM_NONE", "RRQ_NORM_RMS", "RrqNorm", "block_norm",
-    "rrq_block_norm"))
+    "NORM_KINDS", "ROTARY_LAYOUTS", "RRQ_NORM_LAYER", "RRQ_NORM_NONE", "RRQ_NORM_RMS",
+    "RRQ_ROTARY_HALF", "RRQ_ROTARY_INTERLEAVED", "Rotary", "RrqNorm", "RrqRotary", "block_norm",
+    "cache_append", "rotary_frequencies", "rrq_block_norm", "rrq_cache_append"))
 
 
 def __getattr__(name):

@@ -71,3 +71,52 @@ extern "C" int rrq_block_norm(const rrq_norm *norm, const void *residual, int32_
     a.out_bf16 = out_dtype == RRQ_BF16;
     return status(launch_block_norm(a, residual_dtype == RRQ_BF16, y_dtype == RRQ_BF16, stream));
 }
+
+extern "C" int rrq_cache_append(const rrq_cache *cache, const rrq_batch *batch,
+                                const rrq_rotary *rotary, const int32_t *positions, const void *Q,
+                                const void *K, const void *V, int32_t dtype,
+                                int64_t q_token_stride, int64_t q_head_stride,
+                                int64_t k_token_stride, int64_t k_head_stride,
+                                int64_t v_token_stride, int64_t v_head_stride, int32_t n_heads,
+                                void *Q_out, hipStream_t stream)
+{
+    int st = check_cache(cache, true);
+    if (st == RRQ_OK) st = check_batch(batch, true);
+    if (st != RRQ_OK) return st;
+    if (!rotary) return RRQ_ERR_NULL;
+    if (rotary->layout != RRQ_ROTARY_HALF && rotary->layout != RRQ_ROTARY_INTERLEAVED)
+        return RRQ_ERR_FORMAT;
+    if (rotary->rot_dim < 8 || rotary->rot_dim > cache->head_dim || rotary->rot_dim % 8 != 0 ||
+        !std::isfinite(rotary->amplitude) || n_heads < 1 || n_heads > (1 << 16))
+        return RRQ_ERR_SHAPE;
+    if (!known_dtype(dtype)) return RRQ_ERR_DTYPE;
+    if (batch->n_seqs == 0 || batch->n_tokens == 0) return RRQ_OK;
+    if (!rotary->frequencies) return RRQ_ERR_NULL;
+    if (!aligned(rotary->frequencies, 8) || !aligned(positions, 4)) return RRQ_ERR_ALIGN;
+    st = check_rows(Q, dtype, q_token_stride, q_head_stride);
+    if (st == RRQ_OK) st = check_rows(K, dtype, k_token_stride, k_head_stride);
+    if (st == RRQ_OK) st = check_rows(V, dtype, v_token_stride, v_head_stride);
+    if (st != RRQ_OK) return st;
+    if (!Q_out) return RRQ_ERR_NULL;
+    if (!aligned(Q_out, 16)) return RRQ_ERR_ALIGN;
+    CacheAppend a = {};
+    a.cache = *cache;
+    a.batch = *batch;
+    a.K = K;
+    a.V = V;
+    a.Q = Q;
+    a.Q_out = Q_out;
+    a.frequencies = rotary->frequencies;
+    a.positions = positions;
+    a.amplitude = rotary->amplitude;
+    a.k_token = k_token_stride;
+    a.k_head = k_head_stride;
+    a.v_token = v_token_stride;
+    a.v_head = v_head_stride;
+    a.q_token = q_token_stride;
+    a.q_head = q_head_stride;
+    a.n_heads = n_heads;
+    a.rot = rotary->rot_dim;
+    a.interleaved = rotary->layout == RRQ_ROTARY_INTERLEAVED;
+    return status(launch_cache_append(a, dtype == RRQ_BF16, stream));
+}

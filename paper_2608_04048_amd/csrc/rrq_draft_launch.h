@@ -19,4 +19,23 @@ struct BlockNorm {
 };
 hipError_t launch_block_norm(const BlockNorm &a, bool r_bf16, bool y_bf16, hipStream_t stream);
 
+// The append: rows as in CacheWrite, and the queries.
+struct CacheAppend {
+    rrq_cache cache;
+    rrq_batch batch;
+    const void *K, *V, *Q;
+    void *Q_out;
+    const double *frequencies;
+    const int32_t *positions;       // NULL: the rows' places in their sequences
+    double amplitude;
+    int64_t k_token, k_head, v_token, v_head, q_token, q_head;      // strides in elements
+    int32_t n_heads, rot, interleaved;
+    // filled in by the launch: workgroups of pages, tokens a group of queries
+    // has, groups, workgroups that take them
+    int32_t query_tokens;
+    uint32_t page_slots;
+    int64_t query_groups, query_blocks;
+};
+hipError_t launch_cache_append(CacheAppend a, bool bf16, hipStream_t stream);
+
 }  // namespace rrq_detail

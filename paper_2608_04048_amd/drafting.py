@@ -1,11 +1,13 @@
 """What a decoder that drafts tokens with a short prefix of its packages and
 checks them with a longer one runs beside the calls of ``serving``.
 
-Binding of include/rrq_draft.h in librrq.so. ``rrq_block_norm`` marshals
-arguments one to one; ``block_norm`` takes torch tensors, checks them and
-allocates the outputs. Every computation runs in the HIP kernels.
+Binding of include/rrq_draft.h in librrq.so. The functions named like the C ABI
+marshal arguments one to one; the others take torch tensors, check them and
+allocate the outputs. Every computation runs in the HIP kernels.
 
     x, h = block_norm(h, y, weight)          # residual, and rrq_linear's next X
+    rotary = Rotary(rotary_frequencies(128))
+    Q = cache_append(cache, batch, rotary, Q, K, V, positions)
 
 Forward only, and ``stream`` as in ``serving``.
 """
@@ -13,17 +15,22 @@ Forward only, and ``stream`` as in ``serving``.
 from __future__ import annotations
 
 import ctypes
+import math
 
 import torch
 
 from . import RRQ_BF16, RRQ_F32, RRQ_OK, RRQError, _ptr, _stream, load_library
 from .placement import elsewhere, on_stream
-from .serving import _checked, _dtype_code
+from .serving import (CacheBatch, KVCache, _check_out, _checked, _device_index, _dtype_code,
+                      _row_strides)
 
 RRQ_NORM_NONE = 0
 RRQ_NORM_RMS = 1
 RRQ_NORM_LAYER = 2
 NORM_KINDS = {"rms": RRQ_NORM_RMS, "layer": RRQ_NORM_LAYER}
+RRQ_ROTARY_HALF = 0
+RRQ_ROTARY_INTERLEAVED = 1
+ROTARY_LAYOUTS = {"half": RRQ_ROTARY_HALF, "interleaved": RRQ_ROTARY_INTERLEAVED}
 
 
 class RrqNorm(ctypes.Structure):
@@ -31,6 +38,12 @@ class RrqNorm(ctypes.Structure):
     _fields_ = [("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p),
                 ("post_weight", ctypes.c_void_p), ("kind", ctypes.c_int32),
                 ("post", ctypes.c_int32), ("eps", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
+class RrqRotary(ctypes.Structure):
+    """struct rrq_rotary of rrq_draft.h."""
+    _fields_ = [("frequencies", ctypes.c_void_p), ("amplitude", ctypes.c_double),
+                ("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32)]
 
 
 _lib = None
@@ -42,7 +55,9 @@ def _library():
         lib = load_library()
         P, I64, I32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32
         for name, args in (
-                ("rrq_block_norm", [P, P, I32, I64, P, I32, I64, P, I64, I64, I64, P, I32, P, P]),):
+                ("rrq_block_norm", [P, P, I32, I64, P, I32, I64, P, I64, I64, I64, P, I32, P, P]),
+                ("rrq_cache_append", [P, P, P, P, P, P, P, I32, I64, I64, I64, I64, I64, I64, I32,
+                                      P, P])):
             f = getattr(lib, name)
             f.argtypes, f.restype = args, ctypes.c_int
         _lib = lib
@@ -50,7 +65,8 @@ def _library():
 
 
 # ---------------------------------------------------------------------------
-# C ABI, one to one (norm: RrqNorm)
+# C ABI, one to one (cache: RrqCache, batch: RrqBatch, norm: RrqNorm, rotary:
+# RrqRotary)
 # ---------------------------------------------------------------------------
 
 def rrq_block_norm(norm, residual, residual_dtype: int, residual_stride: int, y, y_dtype: int,
@@ -61,6 +77,20 @@ def rrq_block_norm(norm, residual, residual_dtype: int, residual_stride: int, y,
                                        residual_stride, _ptr(y), y_dtype, y_stride, _ptr(gate),
                                        gate_stride, n_rows, hidden, _ptr(out), out_dtype, _ptr(h),
                                        _stream(stream)), "rrq_block_norm")
+
+
+def rrq_cache_append(cache, batch, rotary, positions, Q, K, V, dtype: int, q_token_stride: int,
+                     q_head_stride: int, k_token_stride: int, k_head_stride: int,
+                     v_token_stride: int, v_head_stride: int, n_heads: int, Q_out,
+                     stream=None) -> None:
+    """Enqueue the rotation of a batch's queries and keys and the quantised write of
+    its keys and values (see rrq_draft.h)."""
+    _checked(_library().rrq_cache_append(ctypes.byref(cache), ctypes.byref(batch),
+                                         ctypes.byref(rotary), _ptr(positions), _ptr(Q), _ptr(K),
+                                         _ptr(V), dtype, q_token_stride, q_head_stride,
+                                         k_token_stride, k_head_stride, v_token_stride,
+                                         v_head_stride, n_heads, _ptr(Q_out), _stream(stream)),
+             "rrq_cache_append")
 
 
 # ---------------------------------------------------------------------------
@@ -181,3 +211,84 @@ def block_norm(residual, y=None, weight=None, bias=None, kind: str = "rms", post
     if st != RRQ_OK:
         raise RRQError(st, "rrq_block_norm")
     return x, h
+
+
+def rotary_frequencies(rot_dim: int, base: float = 10000.0, stretch: float = 1.0,
+                       trained: int = 32768, slow: float = 1.0, fast: float = 32.0,
+                       device="cuda"):
+    """float64 [rot_dim / 2]: pair i turns by base ** (-2 i / rot_dim) a position.
+
+    For a context `stretch` times the `trained` one, pairs that turn less than
+    `slow` times in the trained context are slowed by the stretch, those that turn
+    more than `fast` times stay, and between them the share that stays is linear in
+    the turns."""
+    f = base ** (-torch.arange(rot_dim // 2, dtype=torch.float64) * 2 / rot_dim)
+    if stretch != 1.0:
+        stay = ((trained * f / (2 * math.pi) - slow) / (fast - slow)).clamp(0, 1)
+        f = f * stay + f / stretch * (1 - stay)
+    return f.to(device)
+
+
+class Rotary:
+    """Rotary positions: frequencies float64 [rot_dim / 2] on the GPU (radians a
+    position), of which pair i is channels i and i + rot_dim / 2 (layout "half") or
+    2 i and 2 i + 1 ("interleaved") of a head; further channels stay as they are.
+    amplitude multiplies what is rotated."""
+
+    def __init__(self, frequencies, layout: str = "half", amplitude: float = 1.0):
+        if layout not in ROTARY_LAYOUTS:
+            raise ValueError(f"layout must be one of {sorted(ROTARY_LAYOUTS)}, got {layout!r}")
+        if not isinstance(frequencies, torch.Tensor):
+            raise TypeError("frequencies must be a torch.Tensor")
+        if frequencies.dtype != torch.float64:
+            raise TypeError(f"frequencies must have dtype torch.float64, got {frequencies.dtype}")
+        if not frequencies.is_cuda:
+            raise ValueError(f"frequencies must be on a GPU device, got {frequencies.device}")
+        if frequencies.dim() != 1 or not frequencies.is_contiguous():
+            raise ValueError("frequencies must be a contiguous vector")
+        self.frequencies, self.layout, self.amplitude = frequencies, layout, float(amplitude)
+        self.rot_dim = 2 * frequencies.shape[0]
+        self.index = frequencies.get_device()
+        self.desc = RrqRotary(_ptr(frequencies), self.amplitude, self.rot_dim,
+                              ROTARY_LAYOUTS[layout])
+        self.ref = ctypes.byref(self.desc)
+
+
+def _check_positions(positions, rows: int, index: int):
+    """Address of a batch's positions; None for None."""
+    return _vector(positions, "positions", rows, torch.int32, index)
+
+
+def cache_append(cache: KVCache, batch: CacheBatch, rotary: Rotary, Q, K, V, positions=None,
+                 stream=None, out=None):
+    """Rotate the batch's queries [n_tokens, n_heads, head_dim] and keys, and quantise
+    keys and values [n_tokens, n_kv_heads, head_dim] into their pages: float32 or
+    bfloat16, one type, any token and head strides of whole 16 bytes. positions
+    (int32 [n_tokens]) defaults to the rows' places in their sequences. Returns the
+    rotated queries; ``out`` may pass their tensor, Q itself as well."""
+    index = _device_index(cache, batch)
+    if elsewhere(index, stream):
+        used = (*cache.tensors, *batch.tensors, rotary.frequencies, Q, K, V, positions, out)
+        with on_stream(index, stream, *used) as there:
+            return there.returned(cache_append(cache, batch, rotary, Q, K, V, positions, out=out))
+    if rotary.index != index:
+        raise ValueError(f"rotary must be on cuda:{index}, got cuda:{rotary.index}")
+    rows, heads, dim = batch.n_tokens, cache.n_kv_heads, cache.head_dim
+    qt, qh = _row_strides(Q, "Q", rows, None, dim, index)
+    kt, kh = _row_strides(K, "K", rows, heads, dim, index)
+    vt, vh = _row_strides(V, "V", rows, heads, dim, index)
+    dtype = Q.dtype
+    if K.dtype != dtype or V.dtype != dtype:
+        raise TypeError(f"Q, K and V must have one dtype, got {dtype}, {K.dtype} and {V.dtype}")
+    code = _dtype_code(dtype, "Q")
+    at = _check_positions(positions, rows, index)
+    if out is None:
+        out = torch.empty(Q.shape, dtype=dtype, device=cache.device)
+    else:
+        _check_out(out, "out", Q.shape, dtype, index)
+    st = (_lib or _library()).rrq_cache_append(
+        cache.ref, batch.ref, rotary.ref, at, Q.data_ptr(), K.data_ptr(), V.data_ptr(), code,
+        qt, qh, kt, kh, vt, vh, Q.shape[1], out.data_ptr(), _stream(None))
+    if st != RRQ_OK:
+        raise RRQError(st, "rrq_cache_append")
+    return out

@@ -5,10 +5,12 @@ import ctypes
 import os
 import re
 
+import numpy as np
 import pytest
 
 import paper_2608_04048_amd as rrq
 from paper_2608_04048_amd import drafting
+from test_serve_abi import BATCH_CASES, CACHE_CASES, _batch, _cache
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 HEADER = os.path.join(ROOT, "include", "rrq_draft.h")
@@ -18,7 +20,6 @@ FAKE = 0x10000          # aligned, never dereferenced: every case fails validati
 def test_library_exports_every_declared_function():
     text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
     names = sorted(set(re.findall(r"\b(rrq_\w+)\s*\(", text)))
-    assert "rrq_block_norm" in names
     lib = rrq.load_library()
     for name in names:
         assert hasattr(lib, name) and hasattr(rrq, name), name
@@ -28,6 +29,7 @@ def test_library_exports_every_declared_function():
 
 def test_structures_match_the_header():
     assert ctypes.sizeof(rrq.RrqNorm) == 3 * 8 + 4 * 4
+    assert ctypes.sizeof(rrq.RrqRotary) == 2 * 8 + 2 * 4
 
 
 def _ref(x):
@@ -73,3 +75,67 @@ def _norm(norm=_norm_struct(), r=FAKE, rt=0, rs=64, y=FAKE, yt=0, ys=64, gate=FA
 ])
 def test_norm_refusals(kw, status):
     assert _norm(**kw) == status
+
+
+def _rotary(**kw):
+    d = dict(frequencies=FAKE, amplitude=1.0, rot_dim=128, layout=0)
+    d.update(kw)
+    return rrq.RrqRotary(**d)
+
+
+def _append(cache=_cache(), batch=_batch(), rotary=_rotary(), positions=FAKE, Q=FAKE, K=FAKE,
+            V=FAKE, dtype=0, qt=2048, qh=128, kt=2048, kh=128, vt=2048, vh=128, heads=4, out=FAKE):
+    return drafting._library().rrq_cache_append(_ref(cache), _ref(batch), _ref(rotary), positions,
+                                                Q, K, V, dtype, qt, qh, kt, kh, vt, vh, heads,
+                                                out, None)
+
+
+@pytest.mark.parametrize("kw,status", CACHE_CASES)
+def test_cache_descriptor_refusals(kw, status):
+    assert _append(cache=_cache(**kw)) == status
+
+
+@pytest.mark.parametrize("kw,status", BATCH_CASES)
+def test_batch_descriptor_refusals(kw, status):
+    assert _append(batch=_batch(**kw)) == status
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(cache=None), rrq.RRQ_ERR_NULL), (dict(batch=None), rrq.RRQ_ERR_NULL),
+    (dict(rotary=None), rrq.RRQ_ERR_NULL),
+    (dict(rotary=_rotary(frequencies=None)), rrq.RRQ_ERR_NULL),
+    (dict(rotary=_rotary(frequencies=FAKE + 4)), rrq.RRQ_ERR_ALIGN),
+    (dict(rotary=_rotary(rot_dim=0)), rrq.RRQ_ERR_SHAPE),
+    (dict(rotary=_rotary(rot_dim=-8)), rrq.RRQ_ERR_SHAPE),
+    (dict(rotary=_rotary(rot_dim=12)), rrq.RRQ_ERR_SHAPE),
+    (dict(rotary=_rotary(rot_dim=136)), rrq.RRQ_ERR_SHAPE),
+    (dict(rotary=_rotary(layout=2)), rrq.RRQ_ERR_FORMAT),
+    (dict(rotary=_rotary(layout=-1)), rrq.RRQ_ERR_FORMAT),
+    (dict(rotary=_rotary(amplitude=float("inf"))), rrq.RRQ_ERR_SHAPE),
+    (dict(positions=FAKE + 2), rrq.RRQ_ERR_ALIGN), (dict(dtype=2), rrq.RRQ_ERR_DTYPE),
+    (dict(Q=None), rrq.RRQ_ERR_NULL), (dict(K=None), rrq.RRQ_ERR_NULL),
+    (dict(V=None), rrq.RRQ_ERR_NULL), (dict(out=None), rrq.RRQ_ERR_NULL),
+    (dict(Q=FAKE + 4), rrq.RRQ_ERR_ALIGN), (dict(K=FAKE + 8), rrq.RRQ_ERR_ALIGN),
+    (dict(V=FAKE + 2), rrq.RRQ_ERR_ALIGN), (dict(out=FAKE + 8), rrq.RRQ_ERR_ALIGN),
+    (dict(qt=2050), rrq.RRQ_ERR_ALIGN), (dict(dtype=1, kh=132), rrq.RRQ_ERR_ALIGN),
+    (dict(vt=-128), rrq.RRQ_ERR_SHAPE), (dict(heads=0), rrq.RRQ_ERR_SHAPE),
+    (dict(heads=(1 << 16) + 1), rrq.RRQ_ERR_SHAPE),
+    (dict(batch=_batch(n_tokens=0), Q=None, K=None, V=None, out=None), rrq.RRQ_OK),
+    (dict(batch=_batch(n_seqs=0, page_table=None, max_pages=0), Q=None), rrq.RRQ_OK),
+])
+def test_append_refusals(kw, status):
+    assert _append(**kw) == status
+
+
+def test_rotary_frequencies():
+    """Unstretched powers, slow pairs slowed, fast ones kept."""
+    import torch
+    f = rrq.rotary_frequencies(128, device="cpu")
+    assert f.dtype == torch.float64 and np.allclose(f.numpy(), 10000.0 ** (-np.arange(64) / 64), rtol=1e-14)
+    g = rrq.rotary_frequencies(128, stretch=4.0, device="cpu")
+    turns = 32768 * f / (2 * np.pi)
+    assert torch.equal(g[turns >= 32], f[turns >= 32])
+    assert torch.equal(g[turns <= 1], f[turns <= 1] / 4)
+    between = (turns > 1) & (turns < 32)
+    assert between.any() and (g[between] < f[between]).all()
+    assert (g[between] > f[between] / 4).all()
