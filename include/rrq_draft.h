@@ -132,6 +132,34 @@ int rrq_cache_append(const rrq_cache *cache, const rrq_batch *batch, const rrq_r
                      int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
                      int64_t v_head_stride, int32_t n_heads, void *Q_out, hipStream_t stream);
 
+/*
+ * rrq_tree_attention - softmax attention of drafted tokens over the cache, as
+ * rrq_cache_attention, but of its step's own rows a row sees those that its bits say
+ * (its path from the tree's root). A sequence's rows of the batch are at positions
+ * start = length - n_b on in the cache; row i of them sees
+ *   - position j < start, for window > 0 only if j > p_i - window;
+ *   - the step's row j (at start + j) if bit j of row i of `seen` is set, whatever
+ *     the window; a row sees itself by its own bit alone. Bits of n_b and more play
+ *     no part, rows past the bits are not seen.
+ * A row that sees nothing gives zeros.
+ *
+ *   seen       device, uint64 [n_tokens][seen_words], 8-byte aligned: bit j is bit
+ *              j % 64 of word j / 64.
+ *   seen_words 1..2^20.
+ *   positions  device, int32 [n_tokens], 4-byte aligned: p_i, which a window counts
+ *              from (a drafted token's depth in its tree, not its row). NULL: the
+ *              row's place start + i. Not read without a window.
+ *   The other arguments, and the workspace (rrq_cache_attention_workspace), as for
+ *   rrq_cache_attention; and its arithmetic.
+ *
+ * Returns as rrq_cache_attention.
+ */
+int rrq_tree_attention(const rrq_cache *cache, const rrq_batch *batch, const void *Q,
+                       int32_t q_dtype, int64_t q_token_stride, int64_t q_head_stride,
+                       int32_t n_heads, float scale, const uint64_t *seen, int64_t seen_words,
+                       const int32_t *positions, int64_t window, void *out, int32_t out_dtype,
+                       void *workspace, size_t workspace_bytes, hipStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -122,3 +122,33 @@ def append(cache, table, lengths, offsets, positions, frequencies, layout, ampli
     turn = (positions, frequencies, layout, amplitude)
     serving.write(cache, table, lengths, offsets, rotate(K, *turn), V)
     return rotate(Q, *turn)
+
+
+def tree_attention(cache, table, lengths, offsets, Q, seen, positions, scale, window=0):
+    """(out, weight, reach) as serving.attention; seen: for each row the set of its
+    step's rows that it sees."""
+    T, Hq, D = Q.shape
+    ratio = Hq // cache.k.shape[1]
+    out, mean_abs = np.zeros((T, Hq, D)), np.zeros((T, Hq, D))
+    reach = np.zeros((T, Hq))
+    for b, length in enumerate(lengths):
+        n = offsets[b + 1] - offsets[b]
+        start = length - n
+        for h in range(Hq if n > 0 else 0):
+            k = serving.dense(cache, table[b], "k", h // ratio, length)
+            v = serving.dense(cache, table[b], "v", h // ratio, length)
+            for i in range(n):
+                row = offsets[b] + i
+                p = start + i if positions is None else positions[row]
+                keys = [j for j in range(max(start, 0)) if not window or j > p - window]
+                keys += [start + j for j in sorted(seen[row]) if j < n and start + j >= 0]
+                if not keys:
+                    continue
+                q = Q[row, h].astype(np.float64)
+                s = scale * (k[keys] @ q)
+                w = np.exp(s - s.max())
+                w /= w.sum()
+                out[row, h] = w @ v[keys]
+                mean_abs[row, h] = w @ np.abs(v[keys])
+                reach[row, h] = (np.abs(k[keys]) @ np.abs(q)).max()
+    return out, mean_abs, reach

@@ -78,6 +78,78 @@ __device__ __forceinline__ void row_keys(const Attend &a, const RowTile &r, int 
     hi = (int)h;
 }
 
+// Drafted tokens (TREE): row token i sees the cached positions [lo, hi) before the
+// step's own, as far as its window reaches back from its position, and of the step's
+// own those that tree_keys tells.
+__device__ __forceinline__ void row_past(const Attend &a, const RowTile &r, int i, int &lo,
+                                         int &hi)
+{
+    const int h = r.start < 0 ? 0 : (r.start < r.len ? r.start : r.len);
+    int64_t l = 0;
+    if (a.window > 0) {
+        const int64_t at = a.positions ? a.positions[r.o0 + i] : (int64_t)r.start + i;
+        l = at - a.window + 1;
+        l = l < 0 ? 0 : (l > h ? h : l);
+    }
+    lo = (int)l;
+    hi = h;
+}
+
+// Bits from .. to - 1 of 64, both cut to 0..64.
+__device__ __forceinline__ uint64_t bits_between(int from, int to)
+{
+    const uint64_t below = to <= 0 ? 0 : (to >= 64 ? ~0ull : (1ull << to) - 1);
+    return from <= 0 ? below : (from >= 64 ? 0 : below & (~0ull << from));
+}
+
+// Which of the 64 keys from key0 on row token i sees, of what [lo, hi) is its past.
+// Bit j of a row of `seen` is the key of the step's row j, at position start + j.
+__device__ __forceinline__ uint64_t tree_keys(const Attend &a, const RowTile &r, int i, int lo,
+                                              int hi, int key0)
+{
+    uint64_t bits = 0;
+    const int j = key0 - r.start;       // (of the first key; below 0: before the step)
+    if (j > -64) {
+        const uint64_t *row = a.seen + (int64_t)(r.o0 + i) * a.seen_words;
+        const int w = j >> 6, shift = j & 63;
+        if (w >= 0 && w < a.seen_words) bits = row[w] >> shift;
+        if (shift > 0 && w + 1 < a.seen_words) bits |= row[w + 1] << (64 - shift);
+        bits &= bits_between(0, r.len - key0);
+    }
+    return bits | bits_between(lo - key0, hi - key0);
+}
+
+// Keys any row and every row of the tile sees, of drafted tokens: a window's start
+// goes with a row's position, which any row may have.
+template <int R>
+__device__ __forceinline__ void tile_past(const Attend &a, const RowTile &r, int &lo_any,
+                                          int &hi_any, int &lo_all, int &hi_all)
+{
+    int least = 0x7FFFFFFF, most = 0;
+    if (a.window > 0) {
+#pragma unroll
+        for (int k = 0; k < R; k += 64) {
+            const int row = r.row0 + k + (int)(threadIdx.x & (R < 64 ? R - 1 : 63));
+            int lo, hi;
+            row_past(a, r, place_of(a, row < r.n_rows ? row : r.n_rows - 1).token, lo, hi);
+            least = lo < least ? lo : least;
+            most = lo > most ? lo : most;
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int x = __shfl_xor(least, d), y = __shfl_xor(most, d);
+            least = x < least ? x : least;
+            most = y > most ? y : most;
+        }
+    } else {
+        least = 0;
+    }
+    lo_any = uniform(least);
+    lo_all = uniform(most);
+    hi_any = r.len;
+    hi_all = r.start < 0 ? 0 : (r.start < r.len ? r.start : r.len);
+}
+
 // Keys any row and every row of the tile sees: tokens ascend with rows, and so
 // do both ends of what they see.
 template <int R>

@@ -68,8 +68,8 @@ constexpr unsigned few_lds(int D, int waves, int rows)
 constexpr int many_waves(int D) { return D == 64 ? 16 : 8; }
 
 // NW: waves; NQ: blocks of 16 rows of the row tile; PARTS: of an operand
-// (rrq_attention.h).
-template <int D, int CODE, int NW, int NQ, int PARTS>
+// (rrq_attention.h); TREE: rows see of their step what their bits say.
+template <int D, int CODE, int NW, int NQ, int PARTS, bool TREE>
 __global__ __launch_bounds__(64 * NW, NW > 4 || D == 256 || PARTS > 1 ? 1 : 2)
 void attend_kernel(Attend a)
 {
@@ -86,7 +86,10 @@ void attend_kernel(Attend a)
     RowTile r;
     if (!find_rows<R>(a, blockIdx.x, r)) return;
     int lo_any, hi_any, lo_all, hi_all, tb, te;
-    tile_keys<R>(a, r, lo_any, hi_any, lo_all, hi_all);
+    if (TREE)
+        tile_past<R>(a, r, lo_any, hi_any, lo_all, hi_all);
+    else
+        tile_keys<R>(a, r, lo_any, hi_any, lo_all, hi_all);
     const bool alone = split_tiles<R>(a, lo_any, hi_any, split, tb, te);
     if (alone && split > 0) return;
     if (!alone && te <= tb) {
@@ -118,7 +121,10 @@ void attend_kernel(Attend a)
     for (int b = 0; b < NQ; ++b) {
         const int row = r.row0 + 16 * b + col;
         const RowPlace place = place_of(a, row < r.n_rows ? row : r.n_rows - 1);
-        row_keys(a, r, place.token, lo[b], hi[b]);
+        if (TREE)
+            row_past(a, r, place.token, lo[b], hi[b]);
+        else
+            row_keys(a, r, place.token, lo[b], hi[b]);
         float x[KL][16];
         float amax = 0.0f;
         const int64_t at = (int64_t)(r.o0 + place.token) * a.q_token +
@@ -208,14 +214,23 @@ void attend_kernel(Attend a)
         // and value codes of keys that no row sees are cleared.
         if (key0 < lo_all || key0 + kTileKeys > hi_all || !__all(there)) {
 #pragma unroll
-            for (int b = 0; b < NQ; ++b)
+            for (int b = 0; b < NQ; ++b) {
+                uint32_t seen = 0;      // (TREE) a bit for each of the lane's keys
+                if constexpr (TREE) {
+                    const int row = r.row0 + 16 * b + col;
+                    const int token = place_of(a, row < r.n_rows ? row : r.n_rows - 1).token;
+                    seen = (uint32_t)(tree_keys(a, r, token, lo[b], hi[b], key0) >> (16 * g));
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         const int key = orun + 4 * i + c;
-                        if (key < lo[b] || key >= hi[b] || !there) s[b][i][c] = -kInf;
+                        const bool out = TREE ? !((seen >> (4 * i + c)) & 1)
+                                              : key < lo[b] || key >= hi[b];
+                        if (out || !there) s[b][i][c] = -kInf;
                     }
+            }
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
                 uint32_t keep = 0;
@@ -413,7 +428,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Attend a)
     }
 }
 
-template <int D, int CODE, int PARTS>
+template <int D, int CODE, int PARTS, bool TREE>
 hipError_t few_parts(const Attend &a, const AttendPlan &p, hipStream_t stream)
 {
     const dim3 grid((unsigned)attend_row_tiles(a.batch, a.ratio, p.tile), a.cache.n_kv_heads,
@@ -421,13 +436,13 @@ hipError_t few_parts(const Attend &a, const AttendPlan &p, hipStream_t stream)
     // (two parts of heads of 256 pass the registers of a wave of eight)
     constexpr int MANY = D == 256 && PARTS > 1 ? 4 : many_waves(D);
     if (p.waves > 4)
-        attend_kernel<D, CODE, MANY, 1, PARTS>
+        attend_kernel<D, CODE, MANY, 1, PARTS, TREE>
             <<<grid, 64 * MANY, few_lds(D, MANY, a.lds_rows), stream>>>(a);
     else if (p.tile == kWideTile)
-        attend_kernel<D, CODE, 4, D <= 128 ? 2 : 1, PARTS>
+        attend_kernel<D, CODE, 4, D <= 128 ? 2 : 1, PARTS, TREE>
             <<<grid, 256, few_lds(D, 4, a.lds_rows), stream>>>(a);
     else
-        attend_kernel<D, CODE, 4, 1, PARTS>
+        attend_kernel<D, CODE, 4, 1, PARTS, TREE>
             <<<grid, 256, few_lds(D, 4, a.lds_rows), stream>>>(a);
     return hipGetLastError();
 }
@@ -435,7 +450,11 @@ hipError_t few_parts(const Attend &a, const AttendPlan &p, hipStream_t stream)
 template <int D, int CODE>
 hipError_t few_code(const Attend &a, const AttendPlan &p, hipStream_t stream)
 {
-    return a.out_bf16 ? few_parts<D, CODE, 1>(a, p, stream) : few_parts<D, CODE, 2>(a, p, stream);
+    if (a.seen)
+        return a.out_bf16 ? few_parts<D, CODE, 1, true>(a, p, stream)
+                          : few_parts<D, CODE, 2, true>(a, p, stream);
+    return a.out_bf16 ? few_parts<D, CODE, 1, false>(a, p, stream)
+                      : few_parts<D, CODE, 2, false>(a, p, stream);
 }
 
 template <int D>

@@ -74,8 +74,9 @@ __device__ __forceinline__ int channel_of(int slot)
 }
 
 // KEYS: keys of a tile, 32 or 64; PARTS: of an operand (rrq_attention.h), two of
-// which take the registers of a whole wave a SIMD.
-template <int D, int CODE, int KEYS, int PARTS>
+// which take the registers of a whole wave a SIMD; TREE: rows see of their step what
+// their bits say.
+template <int D, int CODE, int KEYS, int PARTS, bool TREE>
 __global__ __launch_bounds__(256, PARTS > 1 ? 1 : 2) void attend_rows_kernel(Attend a)
 {
     // LDS bytes of a row. 16 more than a multiple of 128, so that 8 rows span all
@@ -106,8 +107,13 @@ __global__ __launch_bounds__(256, PARTS > 1 ? 1 : 2) void attend_rows_kernel(Att
     const int64_t token = place.token;
     const int head = kvh * a.ratio + place.member;
     int lo, hi, lo_any, hi_any, lo_all, hi_all;
-    row_keys(a, r, place.token, lo, hi);
-    tile_keys<R>(a, r, lo_any, hi_any, lo_all, hi_all);
+    if (TREE) {
+        row_past(a, r, place.token, lo, hi);
+        tile_past<R>(a, r, lo_any, hi_any, lo_all, hi_all);
+    } else {
+        row_keys(a, r, place.token, lo, hi);
+        tile_keys<R>(a, r, lo_any, hi_any, lo_all, hi_all);
+    }
     int tb, te;
     const bool alone = split_tiles<R>(a, lo_any, hi_any, blockIdx.y, tb, te);
     if (alone && blockIdx.y > 0) return;
@@ -305,12 +311,17 @@ __global__ __launch_bounds__(256, PARTS > 1 ? 1 : 2) void attend_rows_kernel(Att
         if (at_edge(tile) || gone) {
             // -inf stands for a key that the row does not see: its weight is
             // exp2(-inf) = 0
+            uint64_t seen = 0;          // (TREE) a bit for each of the tile's keys
+            if constexpr (TREE)
+                seen = tree_keys(a, r, (int)token, lo, hi, tile * KEYS) >> (4 * hb);
 #pragma unroll
             for (int h = 0; h < NH; ++h)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
-                    const int key = tile * KEYS + 32 * h + 8 * (e >> 2) + 4 * hb + (e & 3);
-                    if (key < lo || key >= hi || ((gone >> (2 * h + (e >> 3))) & 1))
+                    const int at = 32 * h + 8 * (e >> 2) + (e & 3);     // (of the lane's half)
+                    const int key = tile * KEYS + at + 4 * hb;
+                    const bool out = TREE ? !((seen >> at) & 1) : key < lo || key >= hi;
+                    if (out || ((gone >> (2 * h + (e >> 3))) & 1))
                         s[h][e] = -kInf;
                 }
         }
@@ -415,24 +426,30 @@ __global__ __launch_bounds__(256, PARTS > 1 ? 1 : 2) void attend_rows_kernel(Att
         }
 }
 
-template <int D, int CODE>
+template <int D, int CODE, bool TREE>
 hipError_t rows_code(const Attend &a, hipStream_t stream)
 {
     const dim3 grid((unsigned)(attend_row_tiles(a.batch, a.ratio, kRowsTile) *
                                a.cache.n_kv_heads), a.n_splits);
     constexpr int KEYS = D == 256 ? 32 : 64;
     if (a.out_bf16)
-        attend_rows_kernel<D, CODE, KEYS, 1><<<grid, 256, 0, stream>>>(a);
+        attend_rows_kernel<D, CODE, KEYS, 1, TREE><<<grid, 256, 0, stream>>>(a);
     else
-        attend_rows_kernel<D, CODE, KEYS, 2><<<grid, 256, 0, stream>>>(a);
+        attend_rows_kernel<D, CODE, KEYS, 2, TREE><<<grid, 256, 0, stream>>>(a);
     return hipGetLastError();
+}
+
+template <int D, bool TREE>
+hipError_t rows_type(const Attend &a, hipStream_t stream)
+{
+    return a.cache.code_type == RRQ_CODE_INT8 ? rows_code<D, RRQ_CODE_INT8, TREE>(a, stream)
+                                              : rows_code<D, RRQ_CODE_FP8, TREE>(a, stream);
 }
 
 template <int D>
 hipError_t rows_dim(const Attend &a, hipStream_t stream)
 {
-    return a.cache.code_type == RRQ_CODE_INT8 ? rows_code<D, RRQ_CODE_INT8>(a, stream)
-                                              : rows_code<D, RRQ_CODE_FP8>(a, stream);
+    return a.seen ? rows_type<D, true>(a, stream) : rows_type<D, false>(a, stream);
 }
 
 }  // namespace

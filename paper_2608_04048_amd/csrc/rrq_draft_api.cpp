@@ -120,3 +120,26 @@ extern "C" int rrq_cache_append(const rrq_cache *cache, const rrq_batch *batch,
     a.interleaved = rotary->layout == RRQ_ROTARY_INTERLEAVED;
     return status(launch_cache_append(a, dtype == RRQ_BF16, stream));
 }
+
+extern "C" int rrq_tree_attention(const rrq_cache *cache, const rrq_batch *batch, const void *Q,
+                                  int32_t q_dtype, int64_t q_token_stride, int64_t q_head_stride,
+                                  int32_t n_heads, float scale, const uint64_t *seen,
+                                  int64_t seen_words, const int32_t *positions, int64_t window,
+                                  void *out, int32_t out_dtype, void *workspace,
+                                  size_t workspace_bytes, hipStream_t stream)
+{
+    Attend a = {};
+    AttendPlan plan = {};
+    const AttendCall call = {Q, out, workspace, q_token_stride, q_head_stride, window,
+                             workspace_bytes, scale, q_dtype, out_dtype, n_heads, 0};
+    const int st = prepare_attend(cache, batch, call, a, plan);
+    if (st != RRQ_OK) return st;
+    if (seen_words < 1 || seen_words > (int64_t(1) << 20)) return RRQ_ERR_SHAPE;
+    if (plan.splits == 0) return RRQ_OK;
+    if (!seen) return RRQ_ERR_NULL;
+    if (!aligned(seen, 8) || !aligned(positions, 4)) return RRQ_ERR_ALIGN;
+    a.seen = seen;
+    a.seen_words = (int32_t)seen_words;
+    a.positions = positions;
+    return status(launch_attend(a, plan, stream));
+}

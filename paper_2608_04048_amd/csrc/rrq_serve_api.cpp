@@ -12,19 +12,7 @@
 #include "rrq_serve_check.h"
 #include "rrq_serve_launch.h"
 
-namespace {
-
 using namespace rrq_detail;
-
-// Workspace of attention: each split's output (binary32) and its maximum and
-// sum, per row.
-size_t attend_bytes(const rrq_cache *c, const rrq_batch *b, int32_t n_heads, int splits)
-{
-    if (splits == 1) return 0;
-    return (size_t)splits * (size_t)b->n_tokens * (size_t)n_heads * ((size_t)c->head_dim + 2) * 4;
-}
-
-}  // namespace
 
 extern "C" int rrq_cache_write(const rrq_cache *cache, const rrq_batch *batch, const void *K,
                                const void *V, int32_t dtype, int64_t k_token_stride,
@@ -80,44 +68,12 @@ extern "C" int rrq_cache_attention(const rrq_cache *cache, const rrq_batch *batc
                                    int32_t causal, int64_t window, void *out, int32_t out_dtype,
                                    void *workspace, size_t workspace_bytes, hipStream_t stream)
 {
-    int st = check_cache(cache, true);
-    if (st == RRQ_OK) st = check_batch(batch, true);
-    if (st == RRQ_OK) st = check_heads(cache, batch, n_heads);
-    if (st != RRQ_OK) return st;
-    if (!known_dtype(q_dtype) || !known_dtype(out_dtype)) return RRQ_ERR_DTYPE;
-    if (!std::isfinite(scale) || (causal != 0 && causal != 1) || window < 0) return RRQ_ERR_SHAPE;
-    if (batch->n_seqs == 0 || batch->n_tokens == 0) return RRQ_OK;
-    st = check_rows(Q, q_dtype, q_token_stride, q_head_stride);
-    if (st != RRQ_OK) return st;
-    if (!out) return RRQ_ERR_NULL;
-    if (!aligned(out, 16)) return RRQ_ERR_ALIGN;
     Attend a = {};
-    a.cache = *cache;
-    a.batch = *batch;
-    a.Q = Q;
-    a.q_token = q_token_stride;
-    a.q_head = q_head_stride;
-    a.out = out;
-    a.window = window;
-    a.scale = scale;
-    a.n_heads = n_heads;
-    a.ratio = n_heads / cache->n_kv_heads;
-    a.causal = causal;
-    a.q_bf16 = q_dtype == RRQ_BF16;
-    a.out_bf16 = out_dtype == RRQ_BF16;
-    const AttendPlan plan = attend_plan(*cache, *batch, n_heads, window);
-    a.n_splits = plan.splits;
-    a.target = plan.target;
-    a.min_tiles = plan.min_tiles;
-    a.lds_rows = plan.lds_rows;
-    const size_t need = attend_bytes(cache, batch, n_heads, a.n_splits);
-    if (need > 0) {
-        if (!workspace) return RRQ_ERR_NULL;
-        if (!aligned(workspace, 16)) return RRQ_ERR_ALIGN;
-        if (workspace_bytes < need) return RRQ_ERR_WORKSPACE;
-        a.part_o = static_cast<float *>(workspace);
-        a.part_ml = a.part_o + (size_t)a.n_splits * batch->n_tokens * n_heads * cache->head_dim;
-    }
+    AttendPlan plan = {};
+    const AttendCall call = {Q, out, workspace, q_token_stride, q_head_stride, window,
+                             workspace_bytes, scale, q_dtype, out_dtype, n_heads, causal};
+    const int st = prepare_attend(cache, batch, call, a, plan);
+    if (st != RRQ_OK || plan.splits == 0) return st;
     return status(launch_attend(a, plan, stream));
 }
 

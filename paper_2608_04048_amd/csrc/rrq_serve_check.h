@@ -1,11 +1,12 @@
-// Argument checks shared by the C ABI layers of rrq_serve.h and rrq_draft.h.
+// Argument checks, and what calls of attention prepare, shared by the C ABI layers of rrq_serve.h and rrq_draft.h.
 #pragma once
 
+#include <cmath>
 #include <stdint.h>
 
 #include <hip/hip_runtime_api.h>
 
-#include "rrq_serve.h"
+#include "rrq_serve_launch.h"
 
 namespace rrq_detail {
 
@@ -67,6 +68,72 @@ inline int check_heads(const rrq_cache *c, const rrq_batch *b, int32_t n_heads)
 {
     if (n_heads < 1 || n_heads > (1 << 16) || n_heads % c->n_kv_heads != 0) return RRQ_ERR_SHAPE;
     if (b->n_tokens * (n_heads / c->n_kv_heads) > (int64_t(1) << 26)) return RRQ_ERR_SHAPE;
+    return RRQ_OK;
+}
+
+// Workspace of attention: each split's output (binary32) and its maximum and
+// sum, per row.
+inline size_t attend_bytes(const rrq_cache *c, const rrq_batch *b, int32_t n_heads, int splits)
+{
+    if (splits == 1) return 0;
+    return (size_t)splits * (size_t)b->n_tokens * (size_t)n_heads * ((size_t)c->head_dim + 2) * 4;
+}
+
+// A call's arguments besides its cache and batch.
+struct AttendCall {
+    const void *Q;
+    void *out, *workspace;
+    int64_t q_token_stride, q_head_stride, window;
+    size_t workspace_bytes;
+    float scale;
+    int32_t q_dtype, out_dtype, n_heads, causal;
+};
+
+// Checks a call's arguments and fills in what the launch takes. plan.splits stays 0
+// for a call that has nothing to do.
+inline int prepare_attend(const rrq_cache *cache, const rrq_batch *batch, const AttendCall &c,
+                          Attend &a, AttendPlan &plan)
+{
+    int st = check_cache(cache, true);
+    if (st == RRQ_OK) st = check_batch(batch, true);
+    if (st == RRQ_OK) st = check_heads(cache, batch, c.n_heads);
+    if (st != RRQ_OK) return st;
+    if (!known_dtype(c.q_dtype) || !known_dtype(c.out_dtype)) return RRQ_ERR_DTYPE;
+    if (!std::isfinite(c.scale) || (c.causal != 0 && c.causal != 1) || c.window < 0)
+        return RRQ_ERR_SHAPE;
+    if (batch->n_seqs == 0 || batch->n_tokens == 0) return RRQ_OK;
+    st = check_rows(c.Q, c.q_dtype, c.q_token_stride, c.q_head_stride);
+    if (st != RRQ_OK) return st;
+    if (!c.out) return RRQ_ERR_NULL;
+    if (!aligned(c.out, 16)) return RRQ_ERR_ALIGN;
+    a.cache = *cache;
+    a.batch = *batch;
+    a.Q = c.Q;
+    a.q_token = c.q_token_stride;
+    a.q_head = c.q_head_stride;
+    a.out = c.out;
+    a.window = c.window;
+    a.scale = c.scale;
+    a.n_heads = c.n_heads;
+    a.ratio = c.n_heads / cache->n_kv_heads;
+    a.causal = c.causal;
+    a.q_bf16 = c.q_dtype == RRQ_BF16;
+    a.out_bf16 = c.out_dtype == RRQ_BF16;
+    const AttendPlan p = attend_plan(*cache, *batch, c.n_heads, c.window);
+    a.n_splits = p.splits;
+    a.target = p.target;
+    a.min_tiles = p.min_tiles;
+    a.lds_rows = p.lds_rows;
+    const size_t need = attend_bytes(cache, batch, c.n_heads, a.n_splits);
+    if (need > 0) {
+        if (!c.workspace) return RRQ_ERR_NULL;
+        if (!aligned(c.workspace, 16)) return RRQ_ERR_ALIGN;
+        if (c.workspace_bytes < need) return RRQ_ERR_WORKSPACE;
+        a.part_o = static_cast<float *>(c.workspace);
+        a.part_ml =
+            a.part_o + (size_t)a.n_splits * batch->n_tokens * c.n_heads * cache->head_dim;
+    }
+    plan = p;
     return RRQ_OK;
 }
 

@@ -68,7 +68,12 @@ struct Attend {
     float *part_o;      // [n_splits][n_tokens][n_heads][D], n_splits > 1
     float *part_ml;     // [n_splits][n_tokens][n_heads][2]
     int64_t window;     // 0: none
+    // of drafted tokens (NULL: none): which rows of its step each row sees, and the
+    // rows' positions (NULL: their places), which a window counts from
+    const uint64_t *seen;
+    const int32_t *positions;
     float scale;
+    int32_t seen_words;
     int32_t n_heads, ratio, causal, q_bf16, out_bf16;
     int32_t n_splits, target, min_tiles, lds_rows;
 };

@@ -8,6 +8,7 @@ allocate the outputs. Every computation runs in the HIP kernels.
     x, h = block_norm(h, y, weight)          # residual, and rrq_linear's next X
     rotary = Rotary(rotary_frequencies(128))
     Q = cache_append(cache, batch, rotary, Q, K, V, positions)
+    out = tree_attention(cache, batch, Q, seen, positions)
 
 Forward only, and ``stream`` as in ``serving``.
 """
@@ -21,8 +22,8 @@ import torch
 
 from . import RRQ_BF16, RRQ_F32, RRQ_OK, RRQError, _ptr, _stream, load_library
 from .placement import elsewhere, on_stream
-from .serving import (CacheBatch, KVCache, _check_out, _checked, _device_index, _dtype_code,
-                      _row_strides)
+from .serving import (CacheBatch, KVCache, _attention_bytes, _check_out, _checked,
+                      _device_index, _dtype_code, _row_strides, _workspace, _workspace_args)
 
 RRQ_NORM_NONE = 0
 RRQ_NORM_RMS = 1
@@ -54,10 +55,13 @@ def _library():
     if _lib is None:
         lib = load_library()
         P, I64, I32 = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32
+        F, SZ = ctypes.c_float, ctypes.c_size_t
         for name, args in (
                 ("rrq_block_norm", [P, P, I32, I64, P, I32, I64, P, I64, I64, I64, P, I32, P, P]),
                 ("rrq_cache_append", [P, P, P, P, P, P, P, I32, I64, I64, I64, I64, I64, I64, I32,
-                                      P, P])):
+                                      P, P]),
+                ("rrq_tree_attention", [P, P, P, I32, I64, I64, I32, F, P, I64, P, I64, P, I32, P,
+                                        SZ, P])):
             f = getattr(lib, name)
             f.argtypes, f.restype = args, ctypes.c_int
         _lib = lib
@@ -91,6 +95,17 @@ def rrq_cache_append(cache, batch, rotary, positions, Q, K, V, dtype: int, q_tok
                                          k_token_stride, k_head_stride, v_token_stride,
                                          v_head_stride, n_heads, _ptr(Q_out), _stream(stream)),
              "rrq_cache_append")
+
+
+def rrq_tree_attention(cache, batch, Q, q_dtype: int, q_token_stride: int, q_head_stride: int,
+                       n_heads: int, scale: float, seen, seen_words: int, positions, window: int,
+                       out, out_dtype: int, workspace, workspace_bytes: int, stream=None) -> None:
+    """Enqueue attention of drafted tokens over the cache (see rrq_draft.h)."""
+    _checked(_library().rrq_tree_attention(ctypes.byref(cache), ctypes.byref(batch), _ptr(Q),
+                                           q_dtype, q_token_stride, q_head_stride, n_heads, scale,
+                                           _ptr(seen), seen_words, _ptr(positions), window,
+                                           _ptr(out), out_dtype, _ptr(workspace), workspace_bytes,
+                                           _stream(stream)), "rrq_tree_attention")
 
 
 # ---------------------------------------------------------------------------
@@ -291,4 +306,47 @@ def cache_append(cache: KVCache, batch: CacheBatch, rotary: Rotary, Q, K, V, pos
         qt, qh, kt, kh, vt, vh, Q.shape[1], out.data_ptr(), _stream(None))
     if st != RRQ_OK:
         raise RRQError(st, "rrq_cache_append")
+    return out
+
+
+def tree_attention(cache: KVCache, batch: CacheBatch, Q, seen, positions=None, scale=None,
+                   window: int = 0, out_dtype=None, workspace=None, stream=None, out=None):
+    """Attention of drafted tokens, as ``serving.cache_attention`` (with its
+    workspace, ``attention_workspace``): a row sees the positions before its
+    sequence's rows of this batch (of its window, counted from its position), and of
+    those rows the ones whose bits are set in its row of ``seen`` (int64 [n_tokens,
+    words], contiguous: bit j % 64 of word j // 64 is the sequence's row j). positions
+    (int32 [n_tokens]) defaults to the rows' places in their sequences."""
+    index = _device_index(cache, batch)
+    if elsewhere(index, stream):
+        used = (*cache.tensors, *batch.tensors, Q, seen, positions, workspace, out)
+        with on_stream(index, stream, *used) as there:
+            return there.returned(tree_attention(cache, batch, Q, seen, positions, scale, window,
+                                                 out_dtype, workspace, out=out))
+    dim, rows = cache.head_dim, batch.n_tokens
+    qt, qh = _row_strides(Q, "Q", rows, None, dim, index)
+    shape = Q.shape
+    n_heads = shape[1]
+    if (not isinstance(seen, torch.Tensor) or seen.dtype != torch.int64 or
+            seen.get_device() != index or seen.dim() != 2 or seen.shape[0] != rows or
+            not seen.is_contiguous()):
+        raise ValueError(f"seen must be a contiguous int64 tensor [{rows}, words] on cuda:{index}")
+    at = _check_positions(positions, rows, index)
+    if out is None:
+        out_dtype = torch.bfloat16 if out_dtype is None else out_dtype
+        out_code = _dtype_code(out_dtype, "out_dtype")
+        out = torch.empty(shape, dtype=out_dtype, device=cache.device)
+    else:
+        out_dtype = out.dtype if out_dtype is None else out_dtype
+        out_code = _dtype_code(out_dtype, "out")
+        _check_out(out, "out", shape, out_dtype, index)
+    if workspace is None:
+        workspace = _workspace(_attention_bytes(cache, batch, n_heads), cache.device)
+    w, w_bytes = _workspace_args(workspace, index)
+    st = (_lib or _library()).rrq_tree_attention(
+        cache.ref, batch.ref, Q.data_ptr(), _dtype_code(Q.dtype, "Q"), qt, qh, n_heads,
+        1.0 / math.sqrt(dim) if scale is None else scale, seen.data_ptr(), seen.shape[1], at,
+        window, out.data_ptr(), out_code, w, w_bytes, _stream(None))
+    if st != RRQ_OK:
+        raise RRQError(st, "rrq_tree_attention")
     return out

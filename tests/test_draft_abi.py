@@ -139,3 +139,42 @@ def test_rotary_frequencies():
     between = (turns > 1) & (turns < 32)
     assert between.any() and (g[between] < f[between]).all()
     assert (g[between] > f[between] / 4).all()
+
+
+def _tree(cache=_cache(), batch=_batch(), Q=FAKE, dtype=0, qt=1024, qh=128, heads=4, scale=0.1,
+          seen=FAKE, words=1, positions=FAKE, window=0, out=FAKE, out_dtype=1, w=FAKE, wb=1 << 40):
+    return drafting._library().rrq_tree_attention(_ref(cache), _ref(batch), Q, dtype, qt, qh,
+                                                  heads, scale, seen, words, positions, window,
+                                                  out, out_dtype, w, wb, None)
+
+
+@pytest.mark.parametrize("kw,status", CACHE_CASES)
+def test_tree_cache_refusals(kw, status):
+    assert _tree(cache=_cache(**kw)) == status
+
+
+@pytest.mark.parametrize("kw,status", BATCH_CASES)
+def test_tree_batch_refusals(kw, status):
+    assert _tree(batch=_batch(**kw)) == status
+
+
+LONG = _batch(n_seqs=1, n_tokens=1, max_pages=1000, table_stride=1000)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(cache=None), rrq.RRQ_ERR_NULL), (dict(batch=None), rrq.RRQ_ERR_NULL),
+    (dict(Q=None), rrq.RRQ_ERR_NULL), (dict(out=None), rrq.RRQ_ERR_NULL),
+    (dict(seen=None), rrq.RRQ_ERR_NULL), (dict(seen=FAKE + 4), rrq.RRQ_ERR_ALIGN),
+    (dict(words=0), rrq.RRQ_ERR_SHAPE), (dict(words=(1 << 20) + 1), rrq.RRQ_ERR_SHAPE),
+    (dict(positions=FAKE + 2), rrq.RRQ_ERR_ALIGN),
+    (dict(Q=FAKE + 4), rrq.RRQ_ERR_ALIGN), (dict(out=FAKE + 8), rrq.RRQ_ERR_ALIGN),
+    (dict(dtype=2), rrq.RRQ_ERR_DTYPE), (dict(out_dtype=7), rrq.RRQ_ERR_DTYPE),
+    (dict(qt=1026), rrq.RRQ_ERR_ALIGN), (dict(qt=-128), rrq.RRQ_ERR_SHAPE),
+    (dict(heads=3), rrq.RRQ_ERR_SHAPE), (dict(heads=0), rrq.RRQ_ERR_SHAPE),
+    (dict(scale=float("inf")), rrq.RRQ_ERR_SHAPE), (dict(window=-1), rrq.RRQ_ERR_SHAPE),
+    (dict(batch=LONG, w=None), rrq.RRQ_ERR_NULL), (dict(batch=LONG, wb=16), rrq.RRQ_ERR_WORKSPACE),
+    (dict(batch=LONG, w=FAKE + 8), rrq.RRQ_ERR_ALIGN),
+    (dict(batch=_batch(n_tokens=0), Q=None, seen=None, out=None), rrq.RRQ_OK),
+])
+def test_tree_refusals(kw, status):
+    assert _tree(**kw) == status
