@@ -160,6 +160,73 @@ int rrq_tree_attention(const rrq_cache *cache, const rrq_batch *batch, const voi
                        const int32_t *positions, int64_t window, void *out, int32_t out_dtype,
                        void *workspace, size_t workspace_bytes, hipStream_t stream);
 
+/*
+ * rrq_verify_drafts - which drafted tokens the target accepts, and the token that
+ * follows them, from given random numbers.
+ *
+ * Rows offsets[b] .. offsets[b+1]-1 of the logits are sequence b's: row 0 is its last
+ * committed token, row j > 0 the drafted token tokens[j], a child of row parents[j].
+ * p_i is the softmax of row i's logits over the temperature (a temperature of 0: 1 for
+ * the first of the largest logits). A walk starts at row 0 and ends after max_accept
+ * drafts at the latest. At row i its children are tried in the order of their rows:
+ *   - with the draft's distributions (a chain; q_j, the softmax of draft row j - 1 over
+ *     the draft's temperature, is what token j was drawn from): accepted if
+ *     u_j q_j(t_j) < p_i(t_j); else the walk ends, and the next token is drawn from the
+ *     positive part of p_i - q_j (from p_i where that is nothing);
+ *   - without: accepted if u_j w < p_i(t_j), where w is what p_i has left: 1 at first,
+ *     a rejected token's probability is taken out (and is 0 for a sibling with the same
+ *     token). After the last child the walk ends, and the next token is drawn from what
+ *     is left.
+ * Where the walk ends at a row without children, or after max_accept drafts, the next
+ * token is drawn from its p. Drawn is the first token whose running sum, over the
+ * tokens in order, exceeds u_0 times the whole; for a temperature of 0 it is the
+ * likeliest token of the row. At a temperature of 0 draft is not read.
+ *
+ *   logits     device, dtype (RRQ_F32 or RRQ_BF16) [n_rows][vocab], row_stride
+ *              elements between rows, aligned to its type.
+ *   tokens     device, int64 [n_rows], of rows 0 without meaning. One outside the
+ *              vocabulary is rejected.
+ *   offsets    device, int32 [n_seqs + 1], ascending (clamped to 0..n_rows).
+ *   uniforms   device, float [n_rows], in [0, 1): u_j.
+ *   parents    device, int32 [n_rows], by rows within the sequence, 0 <= parents[j] < j
+ *              (another row is no one's child); NULL: a chain, j - 1.
+ *   draft      device, dtype [n_seqs][max_accept][vocab] with strides in elements, or
+ *              NULL. Not together with parents. Rows of absent drafts are not read.
+ *   temperature, draft_temperature  2^-64 .. 2^64; temperature may be 0.
+ *   max_accept 0..2^20.
+ *   counts     device, int32 [n_seqs] (written): accepted drafts.
+ *   following  device, int64 [n_seqs] (written): the next token; -1 for a sequence
+ *              without rows, and where nothing is left to draw from. A row of -inf,
+ *              or one that holds a NaN or +inf, accepts nothing and gives -1 (at a
+ *              temperature of 0 a NaN counts as less than every number).
+ *   paths      device, int32 [n_seqs][max_accept + 1] (written): row 0, then the
+ *              accepted rows, then -1.
+ *   n_rows     0..2^23; vocab 1..2^30; row_stride >= vocab; n_seqs 0..2^20 (0: nothing
+ *              is enqueued); (n_rows + n_seqs (max_accept + 1)) ceil(vocab / 4096) < 2^24.
+ *   workspace  device, 16-byte aligned, workspace_bytes of at least
+ *              rrq_verify_drafts_workspace's value. Its content is of no use before or
+ *              after the call; calls that may run at the same time need their own.
+ * int64 arrays 8-byte aligned, int32 and float arrays 4-byte.
+ *
+ * Arithmetic: the next token is drawn in 64 bits; a row's sum behind an acceptance is
+ * good to about 2^-24. Results are deterministic.
+ *
+ * Returns RRQ_OK, or RRQ_ERR_NULL / _ALIGN / _SHAPE / _DTYPE / _WORKSPACE with nothing
+ * enqueued, or RRQ_ERR_HIP.
+ */
+int rrq_verify_drafts(const void *logits, int32_t dtype, int64_t n_rows, int64_t vocab,
+                      int64_t row_stride, const int64_t *tokens, const int32_t *offsets,
+                      int64_t n_seqs, const float *uniforms, const int32_t *parents,
+                      const void *draft, int64_t draft_seq_stride, int64_t draft_row_stride,
+                      double temperature, double draft_temperature, int32_t max_accept,
+                      int32_t *counts, int64_t *following, int32_t *paths, void *workspace,
+                      size_t workspace_bytes, hipStream_t stream);
+
+/* Bytes of workspace rrq_verify_drafts needs (host only); draft_rows: n_seqs times
+ * max_accept with a draft, else 0. */
+int rrq_verify_drafts_workspace(int64_t n_rows, int64_t vocab, int64_t n_seqs, int64_t draft_rows,
+                                size_t *workspace_bytes);
+
 #ifdef __cplusplus
 }
 #endif

@@ -152,3 +152,80 @@ def tree_attention(cache, table, lengths, offsets, Q, seen, positions, scale, wi
                 mean_abs[row, h] = w @ np.abs(v[keys])
                 reach[row, h] = (np.abs(k[keys]) @ np.abs(q)).max()
     return out, mean_abs, reach
+
+
+def _softmax(x, temperature):
+    """Probabilities of logits x in 64 bits; at a temperature of 0 the first largest."""
+    x = np.asarray(x, np.float64)
+    if temperature == 0:
+        p = np.zeros_like(x)
+        if not np.isnan(x).all():
+            p[int(np.nanargmax(x))] = 1.0
+        return p
+    if np.isnan(x).any() or not np.isfinite(x.max()):
+        return np.full_like(x, np.nan)
+    p = np.exp((x - x.max()) / temperature)
+    return p / p.sum()
+
+
+def verify(logits, tokens, offsets, max_accept, uniforms, draft=None, parents=None,
+           temperature=1.0, draft_temperature=1.0):
+    """(counts, following, paths, margin): margin is how near, relative, any acceptance
+    came to its border; for the token drawn, 10^6 times the share of the whole between
+    the random number and the nearer border (its sums are that much finer)."""
+    counts, following, paths = [], [], []
+    margin = np.inf
+    vocab = logits.shape[1]
+    for b in range(len(offsets) - 1):
+        o, n = offsets[b], max(0, offsets[b + 1] - offsets[b])
+        path = [0] if n else []
+        p = _softmax(logits[o], temperature) if n else None
+        j = 1
+        while j < n and len(path) <= max_accept:
+            i = path[-1]
+            parent = j - 1 if parents is None else int(parents[o + j])
+            if parent != i:
+                j += 1
+                continue
+            t, u = int(tokens[o + j]), float(uniforms[o + j])
+            inside = 0 <= t < vocab
+            if draft is not None and temperature > 0:
+                q = _softmax(draft[b, j - 1], draft_temperature)
+                left, right = u * (q[t] if inside else 0.0), p[t] if inside else 0.0
+                if left < right:
+                    margin = min(margin, (right - left) / max(right, 1e-300))
+                    path.append(j)
+                    p = _softmax(logits[o + j], temperature)
+                    j += 1
+                    continue
+                margin = min(margin, (left - right) / left if left > 0 else np.inf)
+                rest = np.clip(p - q, 0, None)
+                p = rest if np.nansum(rest) > 0 else p
+                break
+            left, right = u * p.sum(), p[t] if inside else 0.0
+            if left < right:
+                margin = min(margin, (right - left) / right)
+                path.append(j)
+                p = _softmax(logits[o + j], temperature)
+            else:
+                if temperature > 0 and left > 0:
+                    margin = min(margin, (left - right) / left)
+                if inside and temperature > 0:
+                    p = p.copy()
+                    p[t] = 0.0
+            j += 1
+        counts.append(max(len(path) - 1, 0))
+        nxt = -1
+        if n and temperature == 0:
+            nxt = int(np.argmax(p)) if p.sum() > 0 else -1
+        elif n and np.isfinite(p.sum()) and p.sum() > 0:
+            total = np.cumsum(p)
+            goal = float(uniforms[o]) * total[-1]
+            above = np.nonzero(total > goal)[0]
+            nxt = int(above[0]) if len(above) else int(np.nonzero(p)[0][-1])
+            margin = min(margin, (total[nxt] - goal) / total[-1] * 1e6,
+                         (goal - (total[nxt] - p[nxt])) / total[-1] * 1e6
+                         if total[nxt] > p[nxt] else np.inf)
+        following.append(nxt)
+        paths.append(path + [-1] * (max_accept + 1 - len(path)))
+    return np.array(counts), np.array(following), np.array(paths), margin

@@ -416,7 +416,8 @@ _DRAFTING = frozenset((
     "NORM_KINDS", "ROTARY_LAYOUTS", "RRQ_NORM_LAYER", "RRQ_NORM_NONE", "RRQ_NORM_RMS",
     "RRQ_ROTARY_HALF", "RRQ_ROTARY_INTERLEAVED", "Rotary", "RrqNorm", "RrqRotary", "block_norm",
     "cache_append", "rotary_frequencies", "rrq_block_norm", "rrq_cache_append", "rrq_tree_attention",
-    "tree_attention"))
+    "rrq_verify_drafts", "rrq_verify_drafts_workspace", "tree_attention", "verify_drafts",
+    "verify_workspace"))
 
 
 def __getattr__(name):

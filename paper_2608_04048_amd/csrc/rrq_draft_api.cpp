@@ -143,3 +143,118 @@ extern "C" int rrq_tree_attention(const rrq_cache *cache, const rrq_batch *batch
     a.positions = positions;
     return status(launch_attend(a, plan, stream));
 }
+
+namespace {
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Logits of a segment of a row: whole blocks, 64 segments at most.
+int64_t verify_segment(int64_t vocab)
+{
+    return ceil_div(ceil_div(vocab, kVerifySumBlock), 64) * kVerifySumBlock;
+}
+
+int check_verify(int64_t n_rows, int64_t vocab, int64_t n_seqs, int64_t draft_rows)
+{
+    if (n_rows < 0 || n_rows > (int64_t(1) << 23) || vocab < 1 || vocab > (int64_t(1) << 30) ||
+        n_seqs < 0 || n_seqs > (int64_t(1) << 20) || draft_rows < 0)
+        return RRQ_ERR_SHAPE;
+    // workgroups of the launches
+    if (draft_rows > (int64_t(1) << 24) ||
+        (n_rows + draft_rows + n_seqs) * ceil_div(vocab, kVerifyDrawBlock) >= (int64_t(1) << 24))
+        return RRQ_ERR_SHAPE;
+    return RRQ_OK;
+}
+
+size_t sums_bytes(int64_t n_rows, int64_t vocab, int64_t draft_rows)
+{
+    return (size_t)(n_rows + draft_rows) * (size_t)ceil_div(vocab, verify_segment(vocab)) *
+           sizeof(VerifySum);
+}
+
+size_t verify_bytes(int64_t n_rows, int64_t vocab, int64_t n_seqs, int64_t draft_rows)
+{
+    return sums_bytes(n_rows, vocab, draft_rows) + (size_t)n_seqs * sizeof(VerifyChoice) +
+           (size_t)n_seqs * (size_t)ceil_div(vocab, kVerifyDrawBlock) * sizeof(VerifyBlock);
+}
+
+bool temperature_fits(double t) { return t >= 0x1p-64 && t <= 0x1p64; }
+
+}  // namespace
+
+extern "C" int rrq_verify_drafts_workspace(int64_t n_rows, int64_t vocab, int64_t n_seqs,
+                                           int64_t draft_rows, size_t *workspace_bytes)
+{
+    if (!workspace_bytes) return RRQ_ERR_NULL;
+    const int st = check_verify(n_rows, vocab, n_seqs, draft_rows);
+    if (st != RRQ_OK) return st;
+    *workspace_bytes = n_seqs == 0 ? 0 : verify_bytes(n_rows, vocab, n_seqs, draft_rows);
+    return RRQ_OK;
+}
+
+extern "C" int rrq_verify_drafts(const void *logits, int32_t dtype, int64_t n_rows, int64_t vocab,
+                                 int64_t row_stride, const int64_t *tokens,
+                                 const int32_t *offsets, int64_t n_seqs, const float *uniforms,
+                                 const int32_t *parents, const void *draft,
+                                 int64_t draft_seq_stride, int64_t draft_row_stride,
+                                 double temperature, double draft_temperature, int32_t max_accept,
+                                 int32_t *counts, int64_t *following, int32_t *paths,
+                                 void *workspace, size_t workspace_bytes, hipStream_t stream)
+{
+    if (max_accept < 0 || max_accept > (1 << 20)) return RRQ_ERR_SHAPE;
+    if (temperature == 0.0 || max_accept == 0) draft = nullptr;
+    // (n_seqs is checked below; the product stays in range before that)
+    const int64_t draft_rows =
+        draft && n_seqs >= 0 && n_seqs <= (int64_t(1) << 20) ? n_seqs * max_accept : 0;
+    const int st = check_verify(n_rows, vocab, n_seqs, draft_rows);
+    if (st != RRQ_OK) return st;
+    if (n_rows > 1 && (row_stride < vocab || row_stride > (int64_t(1) << 36)))
+        return RRQ_ERR_SHAPE;
+    if (!known_dtype(dtype)) return RRQ_ERR_DTYPE;
+    if (temperature != 0.0 && !temperature_fits(temperature)) return RRQ_ERR_SHAPE;
+    if (draft && (parents || !temperature_fits(draft_temperature))) return RRQ_ERR_SHAPE;
+    if (draft && (draft_seq_stride < 0 || draft_row_stride < 0 ||
+                  draft_seq_stride > (int64_t(1) << 40) || draft_row_stride > (int64_t(1) << 36)))
+        return RRQ_ERR_SHAPE;
+    if (n_seqs == 0) return RRQ_OK;
+    if (!offsets || !counts || !following || !paths) return RRQ_ERR_NULL;
+    if (n_rows > 0 && (!logits || !tokens || !uniforms)) return RRQ_ERR_NULL;
+    if (!aligned(logits, size_of(dtype)) || !aligned(draft, size_of(dtype)) ||
+        !aligned(tokens, 8) || !aligned(offsets, 4) || !aligned(uniforms, 4) ||
+        !aligned(parents, 4) || !aligned(counts, 4) || !aligned(following, 8) ||
+        !aligned(paths, 4))
+        return RRQ_ERR_ALIGN;
+    if (!workspace) return RRQ_ERR_NULL;
+    if (!aligned(workspace, 16)) return RRQ_ERR_ALIGN;
+    if (workspace_bytes < verify_bytes(n_rows, vocab, n_seqs, draft_rows))
+        return RRQ_ERR_WORKSPACE;
+    Verify a = {};
+    a.logits = logits;
+    a.draft = draft;
+    a.tokens = tokens;
+    a.offsets = offsets;
+    a.parents = parents;
+    a.uniforms = uniforms;
+    a.counts = counts;
+    a.paths = paths;
+    a.following = following;
+    char *at = static_cast<char *>(workspace);
+    a.sums = reinterpret_cast<VerifySum *>(at);
+    at += sums_bytes(n_rows, vocab, draft_rows);
+    a.choices = reinterpret_cast<VerifyChoice *>(at);
+    a.blocks = reinterpret_cast<VerifyBlock *>(at + (size_t)n_seqs * sizeof(VerifyChoice));
+    a.n_rows = n_rows;
+    a.n_seqs = n_seqs;
+    a.vocab = vocab;
+    a.row_stride = row_stride;
+    a.draft_seq_stride = draft_seq_stride;
+    a.draft_row_stride = draft_row_stride;
+    a.segment = verify_segment(vocab);
+    a.inv_temperature = temperature == 0.0 ? 0.0 : 1.0 / temperature;
+    a.inv_draft_temperature = draft ? 1.0 / draft_temperature : 1.0;
+    a.max_accept = max_accept;
+    a.segments = (int32_t)ceil_div(vocab, a.segment);
+    a.draw_segments = (int32_t)ceil_div(vocab, kVerifyDrawBlock);
+    a.bf16 = dtype == RRQ_BF16;
+    return status(launch_verify(a, stream));
+}

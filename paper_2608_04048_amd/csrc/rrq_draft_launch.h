@@ -38,4 +38,42 @@ struct CacheAppend {
 };
 hipError_t launch_cache_append(CacheAppend a, bool bf16, hipStream_t stream);
 
+// Verification. The workspace: a segment's largest logit and sum (greedy: the place
+// of the largest) of each row; where a sequence's walk ended; sums over a block of the
+// vocabulary of what the next token is drawn from.
+struct VerifySum {
+    float m;
+    int32_t unused;
+    double sum;
+};
+struct VerifyChoice {
+    int32_t row, first, n, at;      // of the logits; of the sequence; -1: no rows
+    int32_t draft;                  // the draft's row that was rejected, -1: none
+    int32_t removed;                // the children's tokens are
+    float m, mq;                    // with a rejected draft: largest logits and sums
+    double l, lq;
+};
+struct VerifyBlock {
+    double p, q, sp, sq;            // of p, of q, of both where p > q
+    float m;                        // p's weights are relative to it
+    int32_t unused;
+};
+struct Verify {
+    const void *logits, *draft;
+    const int64_t *tokens;
+    const int32_t *offsets, *parents;
+    const float *uniforms;
+    int32_t *counts, *paths;
+    int64_t *following;
+    VerifySum *sums;
+    VerifyChoice *choices;
+    VerifyBlock *blocks;
+    int64_t n_rows, n_seqs, vocab, row_stride, draft_seq_stride, draft_row_stride, segment;
+    double inv_temperature, inv_draft_temperature;      // 0: greedy
+    int32_t max_accept, segments, draw_segments, bf16;
+};
+// Logits a workgroup takes at a time; a row's segments are whole blocks, 64 at most.
+constexpr int64_t kVerifySumBlock = 8192, kVerifyDrawBlock = 4096;
+hipError_t launch_verify(const Verify &a, hipStream_t stream);
+
 }  // namespace rrq_detail

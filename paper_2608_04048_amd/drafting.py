@@ -9,6 +9,7 @@ allocate the outputs. Every computation runs in the HIP kernels.
     rotary = Rotary(rotary_frequencies(128))
     Q = cache_append(cache, batch, rotary, Q, K, V, positions)
     out = tree_attention(cache, batch, Q, seen, positions)
+    counts, following, paths = verify_drafts(logits, tokens, offsets, 5, uniforms, draft_logits)
 
 Forward only, and ``stream`` as in ``serving``.
 """
@@ -61,7 +62,10 @@ def _library():
                 ("rrq_cache_append", [P, P, P, P, P, P, P, I32, I64, I64, I64, I64, I64, I64, I32,
                                       P, P]),
                 ("rrq_tree_attention", [P, P, P, I32, I64, I64, I32, F, P, I64, P, I64, P, I32, P,
-                                        SZ, P])):
+                                        SZ, P]),
+                ("rrq_verify_drafts", [P, I32, I64, I64, I64, P, P, I64, P, P, P, I64, I64,
+                                       ctypes.c_double, ctypes.c_double, I32, P, P, P, P, SZ, P]),
+                ("rrq_verify_drafts_workspace", [I64, I64, I64, I64, P])):
             f = getattr(lib, name)
             f.argtypes, f.restype = args, ctypes.c_int
         _lib = lib
@@ -106,6 +110,30 @@ def rrq_tree_attention(cache, batch, Q, q_dtype: int, q_token_stride: int, q_hea
                                            _ptr(seen), seen_words, _ptr(positions), window,
                                            _ptr(out), out_dtype, _ptr(workspace), workspace_bytes,
                                            _stream(stream)), "rrq_tree_attention")
+
+
+def rrq_verify_drafts(logits, dtype: int, n_rows: int, vocab: int, row_stride: int, tokens,
+                      offsets, n_seqs: int, uniforms, parents, draft, draft_seq_stride: int,
+                      draft_row_stride: int, temperature: float, draft_temperature: float,
+                      max_accept: int, counts, following, paths, workspace, workspace_bytes: int,
+                      stream=None) -> None:
+    """Enqueue the verification of drafted tokens (see rrq_draft.h)."""
+    _checked(_library().rrq_verify_drafts(_ptr(logits), dtype, n_rows, vocab, row_stride,
+                                          _ptr(tokens), _ptr(offsets), n_seqs, _ptr(uniforms),
+                                          _ptr(parents), _ptr(draft), draft_seq_stride,
+                                          draft_row_stride, temperature, draft_temperature,
+                                          max_accept, _ptr(counts), _ptr(following), _ptr(paths),
+                                          _ptr(workspace), workspace_bytes, _stream(stream)),
+             "rrq_verify_drafts")
+
+
+def rrq_verify_drafts_workspace(n_rows: int, vocab: int, n_seqs: int, draft_rows: int) -> int:
+    """Bytes of workspace rrq_verify_drafts needs."""
+    n = ctypes.c_size_t(0)
+    _checked(_library().rrq_verify_drafts_workspace(n_rows, vocab, n_seqs, draft_rows,
+                                                    ctypes.byref(n)),
+             "rrq_verify_drafts_workspace")
+    return n.value
 
 
 # ---------------------------------------------------------------------------
@@ -350,3 +378,95 @@ def tree_attention(cache: KVCache, batch: CacheBatch, Q, seen, positions=None, s
     if st != RRQ_OK:
         raise RRQError(st, "rrq_tree_attention")
     return out
+
+
+def _verify_bytes(logits, n_seqs: int, draft) -> int:
+    rows = 0 if draft is None else draft.shape[0] * draft.shape[1]
+    return rrq_verify_drafts_workspace(logits.shape[0], logits.shape[1], n_seqs, rows)
+
+
+def verify_workspace(logits, n_seqs: int, draft=None):
+    """A workspace for verify_drafts on logits and draft distributions of these shapes
+    (uint8 tensor, or None if none is needed). Calls that may run at the same time
+    need their own."""
+    return _workspace(_verify_bytes(logits, n_seqs, draft), logits.device)
+
+
+def verify_drafts(logits, tokens, offsets, max_accept: int, uniforms, draft=None, parents=None,
+                  temperature: float = 1.0, draft_temperature: float = 1.0, workspace=None,
+                  stream=None):
+    """(counts, following, paths): how many drafted tokens of each sequence the target
+    accepts, the token that follows them, and the accepted rows.
+
+    logits [rows, vocab] (float32 or bfloat16, rows may be strided): rows offsets[b] ..
+    offsets[b + 1] - 1 (offsets int32 [n_seqs + 1]) are the target's after sequence b's
+    last token (row 0) and after each drafted one. tokens (int64 [rows]) holds the
+    drafted tokens in rows 1 on, uniforms (float32 [rows], in [0, 1)) a random number
+    for each, and in row 0 the one that the following token is drawn with. parents
+    (int32 [rows], row numbers within the sequence) makes the drafts a tree; without it
+    they are a chain. draft [n_seqs, max_accept, vocab] (a chain's only, of the logits'
+    type) gives the distributions the drafts were drawn from, logits as well; without it
+    a rejected token's probability is taken out. A temperature of 0 is greedy.
+
+    counts is int32 [n_seqs], following int64 [n_seqs] (-1: none), paths int32 [n_seqs,
+    max_accept + 1]: row 0, the accepted rows in order, then -1. At most max_accept
+    drafts of a sequence are accepted."""
+    if not isinstance(logits, torch.Tensor):
+        raise TypeError("logits must be a torch.Tensor")
+    index = logits.get_device()
+    if index < 0:
+        raise ValueError(f"logits must be on a GPU device, got {logits.device}")
+    if elsewhere(index, stream):
+        used = (logits, tokens, offsets, uniforms, draft, parents, workspace)
+        with on_stream(index, stream, *used) as there:
+            return there.returned(verify_drafts(logits, tokens, offsets, max_accept, uniforms,
+                                                draft, parents, temperature, draft_temperature,
+                                                workspace))
+    code = _dtype_code(logits.dtype, "logits")
+    if logits.dim() != 2:
+        raise ValueError(f"logits must be [rows, vocab], got {tuple(logits.shape)}")
+    rows, vocab = logits.shape
+    row_stride = _matrix(logits, "logits", rows, vocab, index)
+    if not isinstance(offsets, torch.Tensor) or offsets.dim() != 1 or offsets.shape[0] < 1:
+        raise ValueError(f"offsets must be a contiguous int32 tensor [n_seqs + 1] on cuda:{index}")
+    n_seqs = offsets.shape[0] - 1
+    token_ptr = _vector(tokens, "tokens", rows, torch.int64, index)
+    offset_ptr = _vector(offsets, "offsets", n_seqs + 1, torch.int32, index)
+    uniform_ptr = _vector(uniforms, "uniforms", rows, torch.float32, index)
+    parent_ptr = _vector(parents, "parents", rows, torch.int32, index)
+    if token_ptr is None or uniform_ptr is None:
+        raise TypeError("tokens and uniforms must be torch.Tensors")
+    if max_accept < 0:
+        raise ValueError(f"max_accept must be 0 or more, got {max_accept}")
+    draft_ptr, seq_stride, draft_stride = None, 0, 0
+    if draft is not None:
+        if parents is not None:
+            raise ValueError("draft distributions need a chain: parents must be None")
+        if not isinstance(draft, torch.Tensor):
+            raise TypeError("draft must be a torch.Tensor")
+        if draft.get_device() != index:
+            raise ValueError(f"draft must be on cuda:{index}, got {draft.device}")
+        if tuple(draft.shape) != (n_seqs, max_accept, vocab):
+            raise ValueError(f"draft must be {(n_seqs, max_accept, vocab)}, got "
+                             f"{tuple(draft.shape)}")
+        if draft.dtype != logits.dtype:
+            raise TypeError(f"draft must have the logits' dtype {logits.dtype}, got {draft.dtype}")
+        seq_stride, draft_stride, one = draft.stride()
+        if one != 1 and vocab > 1:
+            raise ValueError("draft must be contiguous in its last dimension")
+        if draft.numel() > 0:
+            draft_ptr = draft.data_ptr()
+    counts = torch.empty(n_seqs, dtype=torch.int32, device=logits.device)
+    following = torch.empty(n_seqs, dtype=torch.int64, device=logits.device)
+    paths = torch.empty((n_seqs, max_accept + 1), dtype=torch.int32, device=logits.device)
+    if workspace is None:
+        workspace = _workspace(_verify_bytes(logits, n_seqs, draft), logits.device)
+    w, w_bytes = _workspace_args(workspace, index)
+    st = (_lib or _library()).rrq_verify_drafts(
+        logits.data_ptr(), code, rows, vocab, row_stride, token_ptr, offset_ptr, n_seqs,
+        uniform_ptr, parent_ptr, draft_ptr, seq_stride, draft_stride, temperature,
+        draft_temperature, max_accept, counts.data_ptr(), following.data_ptr(), paths.data_ptr(),
+        w, w_bytes, _stream(None))
+    if st != RRQ_OK:
+        raise RRQError(st, "rrq_verify_drafts")
+    return counts, following, paths

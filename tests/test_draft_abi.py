@@ -178,3 +178,51 @@ LONG = _batch(n_seqs=1, n_tokens=1, max_pages=1000, table_stride=1000)
 ])
 def test_tree_refusals(kw, status):
     assert _tree(**kw) == status
+
+
+def _verify(x=FAKE, dtype=0, rows=6, vocab=1000, stride=1000, tokens=FAKE, offsets=FAKE, seqs=2,
+            uniforms=FAKE, parents=None, draft=FAKE, ds=3000, dr=1000, t=1.0, dt=1.0, accept=3,
+            counts=FAKE, following=FAKE, paths=FAKE, w=FAKE, wb=1 << 40):
+    return drafting._library().rrq_verify_drafts(x, dtype, rows, vocab, stride, tokens, offsets,
+                                                 seqs, uniforms, parents, draft, ds, dr, t, dt,
+                                                 accept, counts, following, paths, w, wb, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(x=None), rrq.RRQ_ERR_NULL), (dict(tokens=None), rrq.RRQ_ERR_NULL),
+    (dict(offsets=None), rrq.RRQ_ERR_NULL), (dict(uniforms=None), rrq.RRQ_ERR_NULL),
+    (dict(counts=None), rrq.RRQ_ERR_NULL), (dict(following=None), rrq.RRQ_ERR_NULL),
+    (dict(paths=None), rrq.RRQ_ERR_NULL), (dict(w=None), rrq.RRQ_ERR_NULL),
+    (dict(x=FAKE + 2), rrq.RRQ_ERR_ALIGN), (dict(x=FAKE + 1, dtype=1), rrq.RRQ_ERR_ALIGN),
+    (dict(draft=FAKE + 2), rrq.RRQ_ERR_ALIGN), (dict(tokens=FAKE + 4), rrq.RRQ_ERR_ALIGN),
+    (dict(offsets=FAKE + 2), rrq.RRQ_ERR_ALIGN), (dict(uniforms=FAKE + 1), rrq.RRQ_ERR_ALIGN),
+    (dict(parents=FAKE + 2, draft=None), rrq.RRQ_ERR_ALIGN),
+    (dict(counts=FAKE + 2), rrq.RRQ_ERR_ALIGN), (dict(following=FAKE + 4), rrq.RRQ_ERR_ALIGN),
+    (dict(paths=FAKE + 2), rrq.RRQ_ERR_ALIGN), (dict(w=FAKE + 8), rrq.RRQ_ERR_ALIGN),
+    (dict(dtype=2), rrq.RRQ_ERR_DTYPE), (dict(rows=-1), rrq.RRQ_ERR_SHAPE),
+    (dict(rows=(1 << 23) + 1, vocab=10), rrq.RRQ_ERR_SHAPE), (dict(vocab=0), rrq.RRQ_ERR_SHAPE),
+    (dict(vocab=(1 << 30) + 1), rrq.RRQ_ERR_SHAPE), (dict(stride=999), rrq.RRQ_ERR_SHAPE),
+    (dict(rows=1 << 22, vocab=1 << 17, stride=1 << 17), rrq.RRQ_ERR_SHAPE),
+    (dict(seqs=-1), rrq.RRQ_ERR_SHAPE), (dict(seqs=(1 << 20) + 1), rrq.RRQ_ERR_SHAPE),
+    (dict(accept=-1), rrq.RRQ_ERR_SHAPE), (dict(accept=(1 << 20) + 1), rrq.RRQ_ERR_SHAPE),
+    (dict(seqs=1 << 20, accept=1 << 20), rrq.RRQ_ERR_SHAPE),
+    (dict(parents=FAKE), rrq.RRQ_ERR_SHAPE), (dict(t=-1.0), rrq.RRQ_ERR_SHAPE),
+    (dict(t=float("nan")), rrq.RRQ_ERR_SHAPE), (dict(t=float("inf")), rrq.RRQ_ERR_SHAPE),
+    (dict(t=1e-30), rrq.RRQ_ERR_SHAPE), (dict(dt=0.0), rrq.RRQ_ERR_SHAPE),
+    (dict(ds=-1), rrq.RRQ_ERR_SHAPE), (dict(dr=-1), rrq.RRQ_ERR_SHAPE),
+    (dict(wb=16), rrq.RRQ_ERR_WORKSPACE), (dict(seqs=0, x=None, offsets=None), rrq.RRQ_OK),
+])
+def test_verify_refusals(kw, status):
+    assert _verify(**kw) == status
+
+
+def test_verify_workspace():
+    need = rrq.rrq_verify_drafts_workspace(6, 1000, 2, 6)
+    assert need > rrq.rrq_verify_drafts_workspace(6, 1000, 2, 0) > 0
+    assert _verify(wb=need - 1) == rrq.RRQ_ERR_WORKSPACE
+    assert rrq.rrq_verify_drafts_workspace(6, 1000, 0, 0) == 0
+    for args in ((-1, 5, 1, 0), (1, 0, 1, 0), (1, 5, -1, 0), (1, 5, 1, -1), (1 << 22, 1 << 17, 1, 0)):
+        with pytest.raises(rrq.RRQError) as ei:
+            rrq.rrq_verify_drafts_workspace(*args)
+        assert ei.value.status == rrq.RRQ_ERR_SHAPE
+    assert drafting._library().rrq_verify_drafts_workspace(1, 5, 1, 0, None) == rrq.RRQ_ERR_NULL
