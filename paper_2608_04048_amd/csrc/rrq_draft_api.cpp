@@ -148,12 +148,6 @@ namespace {
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Logits of a segment of a row: whole blocks, 64 segments at most.
-int64_t verify_segment(int64_t vocab)
-{
-    return ceil_div(ceil_div(vocab, kVerifySumBlock), 64) * kVerifySumBlock;
-}
-
 int check_verify(int64_t n_rows, int64_t vocab, int64_t n_seqs, int64_t draft_rows)
 {
     if (n_rows < 0 || n_rows > (int64_t(1) << 23) || vocab < 1 || vocab > (int64_t(1) << 30) ||
@@ -168,7 +162,7 @@ int check_verify(int64_t n_rows, int64_t vocab, int64_t n_seqs, int64_t draft_ro
 
 size_t sums_bytes(int64_t n_rows, int64_t vocab, int64_t draft_rows)
 {
-    return (size_t)(n_rows + draft_rows) * (size_t)ceil_div(vocab, verify_segment(vocab)) *
+    return (size_t)(n_rows + draft_rows) * (size_t)ceil_div(vocab, verify_segment(n_rows + draft_rows, vocab)) *
            sizeof(VerifySum);
 }
 
@@ -202,7 +196,7 @@ extern "C" int rrq_verify_drafts(const void *logits, int32_t dtype, int64_t n_ro
                                  void *workspace, size_t workspace_bytes, hipStream_t stream)
 {
     if (max_accept < 0 || max_accept > (1 << 20)) return RRQ_ERR_SHAPE;
-    if (temperature == 0.0 || max_accept == 0) draft = nullptr;
+    if (max_accept == 0) draft = nullptr;
     // (n_seqs is checked below; the product stays in range before that)
     const int64_t draft_rows =
         draft && n_seqs >= 0 && n_seqs <= (int64_t(1) << 20) ? n_seqs * max_accept : 0;
@@ -212,7 +206,8 @@ extern "C" int rrq_verify_drafts(const void *logits, int32_t dtype, int64_t n_ro
         return RRQ_ERR_SHAPE;
     if (!known_dtype(dtype)) return RRQ_ERR_DTYPE;
     if (temperature != 0.0 && !temperature_fits(temperature)) return RRQ_ERR_SHAPE;
-    if (draft && (parents || !temperature_fits(draft_temperature))) return RRQ_ERR_SHAPE;
+    if (draft && (parents || (temperature != 0.0 && !temperature_fits(draft_temperature))))
+        return RRQ_ERR_SHAPE;
     if (draft && (draft_seq_stride < 0 || draft_row_stride < 0 ||
                   draft_seq_stride > (int64_t(1) << 40) || draft_row_stride > (int64_t(1) << 36)))
         return RRQ_ERR_SHAPE;
@@ -230,7 +225,7 @@ extern "C" int rrq_verify_drafts(const void *logits, int32_t dtype, int64_t n_ro
         return RRQ_ERR_WORKSPACE;
     Verify a = {};
     a.logits = logits;
-    a.draft = draft;
+    a.draft = temperature == 0.0 ? nullptr : draft;
     a.tokens = tokens;
     a.offsets = offsets;
     a.parents = parents;
@@ -249,9 +244,9 @@ extern "C" int rrq_verify_drafts(const void *logits, int32_t dtype, int64_t n_ro
     a.row_stride = row_stride;
     a.draft_seq_stride = draft_seq_stride;
     a.draft_row_stride = draft_row_stride;
-    a.segment = verify_segment(vocab);
+    a.segment = verify_segment(n_rows + draft_rows, vocab);
     a.inv_temperature = temperature == 0.0 ? 0.0 : 1.0 / temperature;
-    a.inv_draft_temperature = draft ? 1.0 / draft_temperature : 1.0;
+    a.inv_draft_temperature = a.draft ? 1.0 / draft_temperature : 1.0;
     a.max_accept = max_accept;
     a.segments = (int32_t)ceil_div(vocab, a.segment);
     a.draw_segments = (int32_t)ceil_div(vocab, kVerifyDrawBlock);

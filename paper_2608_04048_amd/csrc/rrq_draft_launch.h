@@ -72,8 +72,11 @@ struct Verify {
     double inv_temperature, inv_draft_temperature;      // 0: greedy
     int32_t max_accept, segments, draw_segments, bf16;
 };
-// Logits a workgroup takes at a time; a row's segments are whole blocks, 64 at most.
+// Logits a workgroup takes at a time, and the most segments (of whole blocks) of a row.
 constexpr int64_t kVerifySumBlock = 8192, kVerifyDrawBlock = 4096;
+constexpr int kVerifySegments = 64;
+// Logits of a segment where `units` rows are summed.
+int64_t verify_segment(int64_t units, int64_t vocab);
 hipError_t launch_verify(const Verify &a, hipStream_t stream);
 
 }  // namespace rrq_detail

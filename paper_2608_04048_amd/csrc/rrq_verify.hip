@@ -65,6 +65,33 @@ __device__ __forceinline__ double weight(float x, float m, double c)
     return exp2_64(((double)x - (double)m) * c);
 }
 
+// The same from a table of 2^(i / 32) in LDS (no two of which share a bank) and a
+// series of degree 5: half the instructions of the whole one.
+constexpr int kTable = 32;
+__device__ __forceinline__ void fill_table(double *table)
+{
+    if (threadIdx.x < kTable) table[threadIdx.x] = exp2_64(threadIdx.x * (1.0 / kTable));
+    __syncthreads();
+}
+// c: 32 log2(e) / T. The sum with 1.5 2^52 rounds y to a whole number, which its low
+// bits are.
+__device__ __forceinline__ double weight(const double *table, float x, float m, double c)
+{
+    constexpr double kRound = 6755399441055744.0, L = kLn2 / kTable;
+    const double y = ((double)x - (double)m) * c;
+    const double t = y + kRound;
+    const int n = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
+    const double r = y - (t - kRound);
+    double p = L * L * L * L * L / 120.0;
+    p = __builtin_fma(p, r, L * L * L * L / 24.0);
+    p = __builtin_fma(p, r, L * L * L / 6.0);
+    p = __builtin_fma(p, r, L * L / 2.0);
+    p = __builtin_fma(p, r, L);
+    p = __builtin_fma(p, r, 1.0);
+    p = __builtin_amdgcn_ldexp(table[n & (kTable - 1)] * p, n >> 5);
+    return y < -1000.0 * kTable ? 0.0 : p;
+}
+
 __device__ __forceinline__ float logit(const void *row, bool bf16, int64_t i)
 {
     if (bf16) return __uint_as_float((uint32_t)static_cast<const uint16_t *>(row)[i] << 16);
@@ -100,10 +127,18 @@ __device__ __forceinline__ const void *draft_row(const Verify &a, int64_t b, int
            (b * a.draft_seq_stride + j * a.draft_row_stride) * (a.bf16 ? 2 : 4);
 }
 
-// A thread's N logits of the block from `base` on, VEC (16 bytes) in a row each:
-// logit (i * kThreads + thread) * VEC + e of the block is v[i * VEC + e]. -inf past the
-// vocabulary. Rows may start at any multiple of their type.
-template <bool BF16, int N>
+// Where in a block of kThreads * N logits a thread's i-th stands: VEC (16 bytes) in a
+// row; RUNS: N in a row.
+template <bool BF16, int N, bool RUNS>
+__device__ __forceinline__ int place(int i)
+{
+    constexpr int VEC = BF16 ? 8 : 4;
+    return RUNS ? (int)threadIdx.x * N + i : ((i / VEC) * kThreads + (int)threadIdx.x) * VEC + i % VEC;
+}
+
+// A thread's N logits of the block from `base` on. -inf past the vocabulary. Rows may
+// start at any multiple of their type.
+template <bool BF16, bool RUNS, int N>
 __device__ __forceinline__ void load_block(const void *row, int64_t base, int64_t vocab,
                                            float (&v)[N])
 {
@@ -113,7 +148,7 @@ __device__ __forceinline__ void load_block(const void *row, int64_t base, int64_
     const bool whole = base + (int64_t)kThreads * N <= vocab;
 #pragma unroll
     for (int i = 0; i < N / VEC; ++i) {
-        const int64_t at = base + (int64_t)(i * kThreads + (int)threadIdx.x) * VEC;
+        const int64_t at = base + place<BF16, N, RUNS>(i * VEC);
         if (whole || at + VEC <= vocab) {
             const Wide w = *reinterpret_cast<const Wide *>(x + at * SIZE);
 #pragma unroll
@@ -218,50 +253,59 @@ __global__ __launch_bounds__(kThreads) void verify_sums_kernel(Verify a)
     float m = -kInf;
     double sum = 0.0;
     int64_t best = a.vocab;
-    for (int64_t base = (int64_t)seg * a.segment; base < end; base += kSumBlock) {
-        float v[kSumLane];
-        load_block<BF16>(row, base, a.vocab, v);
+    float v[kSumLane];
+    int64_t base = (int64_t)seg * a.segment;
+    load_block<BF16, false>(row, base, a.vocab, v);
+    for (;;) {
+        // the next block is on its way under this one's sums
+        const int64_t next = base + kSumBlock;
+        float w[kSumLane];
+        if (next < end) load_block<BF16, false>(row, next, a.vocab, w);
         float bm = -kInf;
 #pragma unroll
         for (int i = 0; i < kSumLane; ++i) bm = fmaxf(bm, v[i]);
         if (GREEDY) {
             // the first place of a thread's largest (blocks ascend)
-            constexpr int VEC = BF16 ? 8 : 4;
             if (bm > m || best == a.vocab) {
 #pragma unroll
                 for (int i = kSumLane - 1; i >= 0; --i) {
-                    const int64_t at = base + (int64_t)((i / VEC) * kThreads + (int)threadIdx.x) *
-                                                  VEC + i % VEC;
+                    const int64_t at = base + place<BF16, kSumLane, false>(i);
                     if (v[i] == bm && at < a.vocab) best = at;
                 }
                 m = bm;
             }
-            continue;
-        }
-        const float mn = fmaxf(m, block_max(bm, lds_max));
-        const float ms = mn == -kInf ? 0.0f : mn;
-        if (mn > m) sum *= m == -kInf ? 0.0 : exp2_64(((double)m - (double)mn) * c);
-        m = mn;
-        float t = 0.0f;
-        double s = 0.0;
-#pragma unroll
-        for (int i = 0; i < kSumLane; i += 8) {
-            float part = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float d = v[i + e] - ms, w = __builtin_amdgcn_exp2f(d * ch);
-                part += w;
-                // (-inf times 0 is kept out)
-                t = __builtin_fmaf(w, fmaxf(d, -1e30f), t);
+        } else {
+            // a thread's sum is relative to its own largest
+            if (bm > m) {
+                sum *= m == -kInf ? 0.0 : exp2_64(((double)m - (double)bm) * c);
+                m = bm;
             }
-            s += (double)part;
+            const float ms = m == -kInf ? 0.0f : m;
+            float t = 0.0f;
+            double s = 0.0;
+#pragma unroll
+            for (int i = 0; i < kSumLane; i += 8) {
+                float part = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float d = v[i + e] - ms, x = __builtin_amdgcn_exp2f(d * ch);
+                    part += x;
+                    // (-inf times 0 is kept out)
+                    t = __builtin_fmaf(x, fmaxf(d, -1e30f), t);
+                }
+                s += (double)part;
+            }
+            sum += s + kLn2 * cl * (double)t;
         }
-        sum += s + kLn2 * cl * (double)t;
+        if (next >= end) break;
+        base = next;
+#pragma unroll
+        for (int i = 0; i < kSumLane; ++i) v[i] = w[i];
     }
     VerifySum *out = a.sums + unit * a.segments + seg;
+    const float most = block_max(m, lds_max);
     if (GREEDY) {
         // the largest logit, and of equal ones the first
-        const float most = block_max(m, lds_max);
         double at = m == most && best < a.vocab ? (double)best : (double)a.vocab;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) at = fmin(at, __shfl_xor(at, d));
@@ -274,32 +318,56 @@ __global__ __launch_bounds__(kThreads) void verify_sums_kernel(Verify a)
         }
         return;
     }
+    if (m < most && m != -kInf) sum *= exp2_64(((double)m - (double)most) * c);
     sum = block_sum(sum, lds_sum);
-    if (threadIdx.x == 0) *out = VerifySum{m, 0, sum};
+    if (threadIdx.x == 0) *out = VerifySum{most, 0, sum};
 }
 
-// A row's largest logit and sum, from its segments (one thread).
+// A row's largest logit and sum, from its segments, by kRowLanes neighbouring lanes.
+constexpr int kRowLanes = 16;
 __device__ __forceinline__ void row_sum(const Verify &a, int64_t unit, double c, float &m,
                                         double &l)
 {
     const VerifySum *s = a.sums + unit * a.segments;
+    const int lane = threadIdx.x % kRowLanes;
+    constexpr int kMost = kVerifySegments / kRowLanes;
+    VerifySum x[kMost];
     m = -kInf;
-    for (int i = 0; i < a.segments; ++i) m = fmaxf(m, s[i].m);
+#pragma unroll
+    for (int k = 0; k < kMost; ++k) {
+        x[k] = VerifySum{-kInf, 0, 0.0};
+        if (lane + k * kRowLanes < a.segments) x[k] = s[lane + k * kRowLanes];
+        m = fmaxf(m, x[k].m);
+    }
+#pragma unroll
+    for (int d = 1; d < kRowLanes; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
     l = 0.0;
-    for (int i = 0; i < a.segments; ++i)
-        l += s[i].m == -kInf ? s[i].sum : s[i].sum * exp2_64(((double)s[i].m - (double)m) * c);
+#pragma unroll
+    for (int k = 0; k < kMost; ++k)
+        l += x[k].m == -kInf ? x[k].sum
+                             : x[k].sum * exp2_64(((double)x[k].m - (double)m) * c);
+#pragma unroll
+    for (int d = 1; d < kRowLanes; d *= 2) l += __shfl_xor(l, d);
 }
-// A row's first largest logit (one thread); the vocabulary's size for none.
+// A row's first largest logit, by as many lanes; the vocabulary's size for none.
 __device__ __forceinline__ int64_t row_best(const Verify &a, int64_t unit)
 {
     const VerifySum *s = a.sums + unit * a.segments;
     float m = -kInf;
     double at = (double)a.vocab;
-    for (int i = 0; i < a.segments; ++i)
-        if (s[i].sum < (double)a.vocab && (s[i].m > m || at == (double)a.vocab)) {
-            m = s[i].m;
-            at = s[i].sum;
+    auto better = [&](float om, double oat) {
+        if (oat < (double)a.vocab && (at == (double)a.vocab || om > m || (om == m && oat < at))) {
+            m = om;
+            at = oat;
         }
+    };
+    for (int i = threadIdx.x % kRowLanes; i < a.segments; i += kRowLanes) better(s[i].m, s[i].sum);
+#pragma unroll
+    for (int d = 1; d < kRowLanes; d *= 2) {
+        const float om = __shfl_xor(m, d);
+        const double oat = __shfl_xor(at, d);
+        better(om, oat);
+    }
     return (int64_t)at;
 }
 
@@ -312,79 +380,99 @@ __device__ __forceinline__ double lane_value(double x, int i)
     return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 
-// Step 2: one wave a sequence.
-__global__ __launch_bounds__(64) void verify_decide_kernel(Verify a)
+// Step 2: one workgroup a sequence. Of 64 rows at a time, kRowLanes lanes a row find
+// the token's probability under its parent; the first wave walks.
+__global__ __launch_bounds__(kThreads) void verify_decide_kernel(Verify a)
 {
-    const int b = blockIdx.x, lane = threadIdx.x;
-    const bool greedy = a.inv_temperature == 0.0;
+    struct Row {
+        double w, q, l, lq;
+        float m, mq;
+    };
+    __shared__ Row rows[64];
+    __shared__ int at_shared, count_shared, rejected_shared;
+    const int b = blockIdx.x, t = threadIdx.x, lane = t & 63;
+    const bool greedy = a.inv_temperature == 0.0, given = a.draft && !greedy;
     int n;
     const int o0 = rows_of(a, b, n);
     int32_t *path = a.paths + (int64_t)b * (a.max_accept + 1);
-    for (int i = lane; i <= a.max_accept; i += 64) path[i] = i == 0 && n > 0 ? 0 : -1;
+    for (int i = t; i <= a.max_accept; i += kThreads) path[i] = i == 0 && n > 0 ? 0 : -1;
     const double c = kLog2e * a.inv_temperature, cq = kLog2e * a.inv_draft_temperature;
     int at = 0, count = 0, rejected = -1;
     double mass = 1.0;
-    for (int base = 0; base < n && count < a.max_accept; base += 64) {
-        // this lane's row: its token's probability w under its parent, and q
-        const int j = base + lane;
-        const int parent = j < n ? parent_of(a, o0, j) : -1;
-        double w = 0.0, q = 1.0, u = 0.0;
-        int64_t token = -1;
-        if (parent >= 0) {
-            token = a.tokens[o0 + j];
-            u = (double)a.uniforms[o0 + j];
+    for (int base = 0; base < n && count < a.max_accept && rejected < 0; base += 64) {
+        for (int k = t / kRowLanes; k < 64 && base + k < n; k += kThreads / kRowLanes) {
+            const int j = base + k, parent = parent_of(a, o0, j);
+            if (parent < 0) continue;
+            const int64_t token = a.tokens[o0 + j];
             const bool inside = token >= 0 && token < a.vocab;
+            Row r = {};
             if (greedy) {
-                w = inside && token == row_best(a, o0 + parent) ? 1.0 : 0.0;
+                r.w = token == row_best(a, o0 + parent) && inside ? 1.0 : 0.0;
             } else {
                 const float x = inside ? logit(target_row(a, o0 + parent), a.bf16, token) : -kInf;
-                float m;
-                double l;
-                row_sum(a, o0 + parent, c, m, l);
-                w = weight(x, m, c) / l;
-                if (a.draft) {
-                    q = 0.0;
-                    if (j <= a.max_accept) {
-                        const float y = inside ? logit(draft_row(a, b, j - 1), a.bf16, token)
-                                               : -kInf;
-                        row_sum(a, a.n_rows + (int64_t)b * a.max_accept + j - 1, cq, m, l);
-                        q = weight(y, m, cq) / l;
-                    }
+                float y = -kInf;
+                if (given && j <= a.max_accept) {
+                    if (inside) y = logit(draft_row(a, b, j - 1), a.bf16, token);
+                    row_sum(a, a.n_rows + (int64_t)b * a.max_accept + j - 1, cq, r.mq, r.lq);
+                    r.q = inside ? weight(y, r.mq, cq) / r.lq : 0.0;
                 }
-                if (!inside) w = 0.0;
+                row_sum(a, o0 + parent, c, r.m, r.l);
+                r.w = inside ? weight(x, r.m, c) / r.l : 0.0;
+            }
+            if (t % kRowLanes == 0) rows[k] = r;
+        }
+        // (the path's first entries are written before the walk's)
+        __syncthreads();
+        if (t < 64) {
+            const int j = base + lane;
+            const int parent = j < n ? parent_of(a, o0, j) : -1;
+            double w = 0.0, q = 0.0, u = 0.0;
+            int64_t token = -1;
+            if (parent >= 0) {
+                w = rows[lane].w;
+                q = rows[lane].q;
+                token = a.tokens[o0 + j];
+                u = (double)a.uniforms[o0 + j];
+            }
+            // a token that an earlier sibling has was rejected there: by rows of
+            // earlier rounds, and below by those of this one
+            for (int k0 = at & ~63; a.parents && k0 < base; k0 += 64) {
+                const bool sibling = parent_of(a, o0, k0 + lane) == at;
+                const int64_t gone = sibling ? a.tokens[o0 + k0 + lane] : -1;
+                for (uint64_t left = __ballot(sibling); left; left &= left - 1)
+                    if (token == __shfl(gone, __builtin_ctzll(left)) && parent == at) w = 0.0;
+            }
+            uint64_t tried = __ballot(parent == at);
+            while (tried) {
+                const int i = __builtin_ctzll(tried);
+                const double wi = lane_value(w, i), ui = lane_value(u, i);
+                if (given ? ui * lane_value(q, i) < wi : ui * mass < wi) {
+                    at = base + i;
+                    mass = 1.0;
+                    ++count;
+                    if (lane == 0) path[count] = at;
+                    if (count == a.max_accept) break;
+                    tried = __ballot(parent == at);
+                    continue;
+                }
+                if (given) {
+                    rejected = base + i;
+                    break;
+                }
+                mass -= wi;
+                tried &= tried - 1;
+                if (parent == at && token == __shfl(token, i)) w = 0.0;
+            }
+            if (lane == 0) {
+                at_shared = at;
+                count_shared = count;
+                rejected_shared = rejected;
             }
         }
-        // a token that an earlier sibling has was rejected there: by rows of earlier
-        // rounds, and below by those of this one
-        for (int k0 = at & ~63; a.parents && k0 < base; k0 += 64) {
-            const bool sibling = parent_of(a, o0, k0 + lane) == at;
-            const int64_t gone = sibling ? a.tokens[o0 + k0 + lane] : -1;
-            for (uint64_t left = __ballot(sibling); left; left &= left - 1)
-                if (token == __shfl(gone, __builtin_ctzll(left)) && parent == at) w = 0.0;
-        }
-        uint64_t tried = __ballot(parent == at);
-        while (tried) {
-            const int i = __builtin_ctzll(tried);
-            const double wi = lane_value(w, i), ui = lane_value(u, i);
-            const bool accept = a.draft && !greedy ? ui * lane_value(q, i) < wi : ui * mass < wi;
-            if (accept) {
-                at = base + i;
-                mass = 1.0;
-                ++count;
-                if (lane == 0) path[count] = at;
-                if (count == a.max_accept) break;
-                tried = __ballot(parent == at);
-                continue;
-            }
-            if (a.draft && !greedy) {
-                rejected = base + i;
-                break;
-            }
-            mass -= wi;
-            tried &= tried - 1;
-            if (parent == at && token == __shfl(token, i)) w = 0.0;
-        }
-        if (rejected >= 0) break;
+        __syncthreads();
+        at = at_shared;
+        count = count_shared;
+        rejected = rejected_shared;
     }
     VerifyChoice choice = {};
     choice.row = n > 0 ? o0 + at : -1;
@@ -393,77 +481,72 @@ __global__ __launch_bounds__(64) void verify_decide_kernel(Verify a)
     choice.at = at;
     choice.draft = rejected >= 0 ? rejected - 1 : -1;
     // children were all tried and rejected
-    choice.removed = !a.draft && count < a.max_accept;
-    if (lane == 0) {
+    choice.removed = !given && count < a.max_accept;
+    if (rejected >= 0) {
+        const Row &r = rows[rejected & 63];
+        choice.m = r.m;
+        choice.l = r.l;
+        choice.mq = r.mq;
+        choice.lq = r.lq;
+    }
+    int64_t following = -1;
+    if (greedy && n > 0) {
+        following = row_best(a, choice.row);
+        if (following >= a.vocab) following = -1;
+    }
+    if (t == 0) {
         a.counts[b] = count;
-        if (greedy || n == 0) {
-            const int64_t t = n > 0 ? row_best(a, choice.row) : a.vocab;
-            a.following[b] = t < a.vocab ? t : -1;
-        }
-        if (rejected >= 0) {
-            float m;
-            double l;
-            row_sum(a, choice.row, c, m, l);
-            choice.m = m;
-            choice.l = l;
-            row_sum(a, a.n_rows + (int64_t)b * a.max_accept + choice.draft, cq, m, l);
-            choice.mq = m;
-            choice.lq = l;
-        }
+        if (greedy || n == 0) a.following[b] = following;
         a.choices[b] = choice;
     }
 }
 
-// Weights of a thread's logits of block `seg` of the sequence's row: w[i], of v[i] less m.
-// With a rejected draft also q's.
+// Weights w of a thread's logits of block `seg` of the sequence's row, relative to the
+// logit m, and with a rejected draft the draft's, q. RUNS: as in place().
 struct Weights {
     double w[kDrawLane], q[kDrawLane];
-    float m;
 };
-template <bool BF16>
-__device__ __forceinline__ void load_weights(const Verify &a, int b, const VerifyChoice &c, int seg,
-                                             float ref, bool given, float *lds, Weights &r)
+template <bool BF16, bool RUNS>
+__device__ __forceinline__ void load_logits(const Verify &a, int b, const VerifyChoice &c, int seg,
+                                            float (&v)[kDrawLane], float (&y)[kDrawLane])
 {
-    constexpr int VEC = BF16 ? 8 : 4;
-    const int64_t base = (int64_t)seg * kDrawBlock;
-    float v[kDrawLane], y[kDrawLane];
-    load_block<BF16>(target_row(a, c.row), base, a.vocab, v);
-    if (c.draft >= 0) load_block<BF16>(draft_row(a, b, c.draft), base, a.vocab, y);
-    r.m = ref;
-    if (!given) {
-        float bm = -kInf;
+    load_block<BF16, RUNS>(target_row(a, c.row), (int64_t)seg * kDrawBlock, a.vocab, v);
+    if (c.draft >= 0)
+        load_block<BF16, RUNS>(draft_row(a, b, c.draft), (int64_t)seg * kDrawBlock, a.vocab, y);
+}
+template <bool BF16, bool RUNS>
+__device__ __forceinline__ void make_weights(const Verify &a, const VerifyChoice &c, int seg,
+                                             const float (&v)[kDrawLane],
+                                             const float (&y)[kDrawLane], float m,
+                                             const double *table, Weights &r)
+{
+    const float ms = m == -kInf ? 0.0f : m;
+    const double f = kTable * kLog2e * a.inv_temperature;
 #pragma unroll
-        for (int i = 0; i < kDrawLane; ++i) bm = fmaxf(bm, v[i]);
-        r.m = block_max(bm, lds);
-    }
-    const float ms = r.m == -kInf ? 0.0f : r.m;
-    const double f = kLog2e * a.inv_temperature;
-#pragma unroll
-    for (int i = 0; i < kDrawLane; ++i) r.w[i] = weight(v[i], ms, f);
+    for (int i = 0; i < kDrawLane; ++i) r.w[i] = weight(table, v[i], ms, f);
     if (c.draft >= 0) {
-        const double fq = kLog2e * a.inv_draft_temperature;
+        const double fq = kTable * kLog2e * a.inv_draft_temperature;
 #pragma unroll
-        for (int i = 0; i < kDrawLane; ++i) r.q[i] = weight(y[i], c.mq, fq);
+        for (int i = 0; i < kDrawLane; ++i) r.q[i] = weight(table, y[i], c.mq, fq);
     }
-    if (c.removed) {
-        // children of the row: 64 at a time, each wave on its own
-        const int lane = threadIdx.x & 63;
-        for (int k0 = c.at + 1; k0 < c.n; k0 += 64) {
-            const int k = k0 + lane;
-            int64_t token = -1;
-            if (k < c.n && parent_of(a, c.first, k) == c.at) token = a.tokens[c.first + k];
-            uint64_t here = __ballot(token >= base && token < base + kDrawBlock);
-            while (here) {
-                const int i = __builtin_ctzll(here);
-                here &= here - 1;
-                const int at = (int)(__shfl(token, i) - base);
+    if (!c.removed) return;
+    // children of the row: 64 at a time, each wave on its own
+    const int64_t base = (int64_t)seg * kDrawBlock;
+    const int lane = threadIdx.x & 63;
+    for (int k0 = c.at + 1; k0 < c.n; k0 += 64) {
+        const int k = k0 + lane;
+        int64_t token = -1;
+        if (k < c.n && parent_of(a, c.first, k) == c.at) token = a.tokens[c.first + k];
+        uint64_t here = __ballot(token >= base && token < base + kDrawBlock);
+        while (here) {
+            const int i = __builtin_ctzll(here);
+            here &= here - 1;
+            const int at = (int)(__shfl(token, i) - base);
 #pragma unroll
-                for (int e = 0; e < kDrawLane; ++e)
-                    if (at == ((e / VEC) * kThreads + (int)threadIdx.x) * VEC + e % VEC)
-                        r.w[e] = 0.0;
-            }
-            if (!a.parents) break;      // a chain's row has one child, the next
+            for (int e = 0; e < kDrawLane; ++e)
+                if (at == place<BF16, kDrawLane, RUNS>(e)) r.w[e] = 0.0;
         }
+        if (!a.parents) break;      // a chain's row has one child, the next
     }
 }
 
@@ -472,13 +555,23 @@ template <bool BF16>
 __global__ __launch_bounds__(kThreads) void verify_weights_kernel(Verify a)
 {
     __shared__ float lds_max[kWaves];
-    __shared__ double lds[kWaves];
+    __shared__ double lds[4][kWaves], table[kTable];
     const int b = blockIdx.x / (uint32_t)a.draw_segments;
     const int seg = blockIdx.x % (uint32_t)a.draw_segments;
     const VerifyChoice c = a.choices[b];
     if (c.row < 0) return;
+    float v[kDrawLane], y[kDrawLane];
+    load_logits<BF16, false>(a, b, c, seg, v, y);
+    fill_table(table);
+    float m = c.m;
+    if (c.draft < 0) {
+        m = -kInf;
+#pragma unroll
+        for (int i = 0; i < kDrawLane; ++i) m = fmaxf(m, v[i]);
+        m = block_max(m, lds_max);
+    }
     Weights r;
-    load_weights<BF16>(a, b, c, seg, c.m, c.draft >= 0, lds_max, r);
+    make_weights<BF16, false>(a, c, seg, v, y, m, table, r);
     double p = 0.0, q = 0.0, sp = 0.0, sq = 0.0;
 #pragma unroll
     for (int i = 0; i < kDrawLane; ++i) p += r.w[i];
@@ -491,13 +584,29 @@ __global__ __launch_bounds__(kThreads) void verify_weights_kernel(Verify a)
                 sq += r.q[i];
             }
         }
-        q = block_sum(q, lds);
-        sp = block_sum(sp, lds);
-        sq = block_sum(sq, lds);
+        q = wave_sum(q);
+        sp = wave_sum(sp);
+        sq = wave_sum(sq);
     }
-    p = block_sum(p, lds);
-    if (threadIdx.x == 0)
-        a.blocks[(int64_t)b * a.draw_segments + seg] = VerifyBlock{p, q, sp, sq, r.m, 0};
+    p = wave_sum(p);
+    if ((threadIdx.x & 63) == 0) {
+        const int w = threadIdx.x >> 6;
+        lds[0][w] = p;
+        lds[1][w] = q;
+        lds[2][w] = sp;
+        lds[3][w] = sq;
+    }
+    __syncthreads();
+    if (threadIdx.x > 0) return;
+    double all[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        all[i] = lds[i][0];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) all[i] += lds[i][w];
+    }
+    a.blocks[(int64_t)b * a.draw_segments + seg] =
+        VerifyBlock{all[0], all[1], all[2], all[3], m, 0};
 }
 
 // Inclusive sum over the workgroup's threads; total: of all.
@@ -522,21 +631,50 @@ __device__ __forceinline__ double block_scan(double x, double *lds, double &tota
     return before + x;
 }
 
+// The first thread that has `is`, of it `at`, and the last that has `was`, of it `to`;
+// `none` and -1 for none. Places ascend with threads.
+__device__ __forceinline__ void first_and_last(bool is, int at, bool was, int to, int none,
+                                               int (*lds)[kWaves], int &first, int &last)
+{
+    const int wave = threadIdx.x >> 6;
+    const uint64_t i = __ballot(is), w = __ballot(was);
+    const int f = i ? __shfl(at, __builtin_ctzll(i)) : none;
+    const int l = w ? __shfl(to, 63 - __builtin_clzll(w)) : -1;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) {
+        lds[0][wave] = f;
+        lds[1][wave] = l;
+    }
+    __syncthreads();
+    first = none;
+    last = -1;
+#pragma unroll
+    for (int k = 0; k < kWaves; ++k) {
+        first = lds[0][k] < first ? lds[0][k] : first;
+        last = lds[1][k] > last ? lds[1][k] : last;
+    }
+}
+
 // Step 4: one workgroup a sequence.
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void verify_draw_kernel(Verify a)
 {
     __shared__ float lds_max[kWaves];
-    __shared__ double lds[kWaves];
-    __shared__ int picked, last;
+    __shared__ double lds[kWaves], table[kTable];
+    __shared__ int lds_place[2][kWaves];
     __shared__ double before_picked;
     const int b = blockIdx.x, t = threadIdx.x;
     const VerifyChoice c = a.choices[b];
     if (c.row < 0) return;
     const VerifyBlock *blocks = a.blocks + (int64_t)b * a.draw_segments;
     const double f = kLog2e * a.inv_temperature;
-    float m = -kInf;
-    for (int i = t; i < a.draw_segments; i += kThreads) m = fmaxf(m, blocks[i].m);
+    // this thread's block of the first round, read once
+    VerifyBlock mine = {0.0, 0.0, 0.0, 0.0, -kInf, 0};
+    if (t < a.draw_segments) mine = blocks[t];
+    fill_table(table);
+    auto block = [&](int i) { return i < kThreads ? mine : blocks[i]; };
+    float m = mine.m;
+    for (int i = t + kThreads; i < a.draw_segments; i += kThreads) m = fmaxf(m, blocks[i].m);
     m = block_max(m, lds_max);
     // a block's weights relative to the row's largest logit
     auto whole = [&](const VerifyBlock &k) {
@@ -544,97 +682,80 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(Verify a)
     };
     double lp = 0.0, lq = 0.0, res = 0.0;
     for (int i = t; i < a.draw_segments; i += kThreads) {
-        lp += whole(blocks[i]);
-        lq += blocks[i].q;
+        const VerifyBlock k = block(i);
+        lp += whole(k);
+        lq += k.q;
     }
     lp = block_sum(lp, lds);
     bool residual = c.draft >= 0;
     if (residual) {
         lq = block_sum(lq, lds);
-        for (int i = t; i < a.draw_segments; i += kThreads)
-            res += fmax(blocks[i].sp / lp - blocks[i].sq / lq, 0.0);
+        for (int i = t; i < a.draw_segments; i += kThreads) {
+            const VerifyBlock k = block(i);
+            res += fmax(k.sp / lp - k.sq / lq, 0.0);
+        }
         res = block_sum(res, lds);
         residual = res > 0.0;           // (else p itself)
     }
-    auto of_block = [&](const VerifyBlock &k) {
-        return residual ? fmax(k.sp / lp - k.sq / lq, 0.0) : whole(k);
-    };
     const double total = residual ? res : lp;
-    if (t == 0) {
-        picked = a.draw_segments;
-        last = -1;
-    }
-    __syncthreads();
     if (!(total > 0.0) || total > 1e300) {
         if (t == 0) a.following[b] = -1;
         return;
     }
     const double goal = (double)a.uniforms[c.first] * total;
     // the first block past which the sum exceeds the goal, the last that has any
+    int seg = a.draw_segments, last = -1;
     double before = 0.0;
-    for (int i0 = 0; i0 < a.draw_segments; i0 += kThreads) {
+    for (int i0 = 0; i0 < a.draw_segments && seg == a.draw_segments; i0 += kThreads) {
         const int i = i0 + t;
-        const double x = i < a.draw_segments ? of_block(blocks[i]) : 0.0;
+        double x = 0.0;
+        if (i < a.draw_segments) {
+            const VerifyBlock k = block(i);
+            x = residual ? fmax(k.sp / lp - k.sq / lq, 0.0) : whole(k);
+        }
         double sum;
         const double upto = before + block_scan(x, lds, sum);
-        if (x > 0.0) {
-            atomicMax(&last, i);
-            if (upto > goal) atomicMin(&picked, i);
-        }
-        __syncthreads();
-        if (picked < a.draw_segments) {
-            if (i == picked) before_picked = upto - x;
-            break;
-        }
+        int some;
+        first_and_last(x > 0.0 && upto > goal, i, x > 0.0, i, a.draw_segments, lds_place, seg,
+                       some);
+        last = some >= 0 ? some : last;
+        if (i == seg) before_picked = upto - x;
         before += sum;
     }
     __syncthreads();
     // a goal past the sum's last digit: the last token that has any weight
-    const bool past = picked >= a.draw_segments;
-    const int seg = past ? last : picked;
+    const bool past = seg == a.draw_segments;
+    if (past) seg = last;
     if (seg < 0) {
         if (t == 0) a.following[b] = -1;
         return;
     }
-    const double start = past ? 0.0 : before_picked;
+    float v[kDrawLane], y[kDrawLane];
+    load_logits<BF16, true>(a, b, c, seg, v, y);
     Weights r;
-    load_weights<BF16>(a, b, c, seg, m, true, lds_max, r);
+    make_weights<BF16, true>(a, c, seg, v, y, m, table, r);
     if (residual) {
 #pragma unroll
         for (int i = 0; i < kDrawLane; ++i)
             r.w[i] = r.w[i] * c.lq > r.q[i] * c.l ? fmax(r.w[i] / lp - r.q[i] / lq, 0.0) : 0.0;
     }
-    // pieces of VEC logits a thread, in the order of the vocabulary
-    constexpr int VEC = BF16 ? 8 : 4;
-    __syncthreads();
-    if (t == 0) {
-        picked = kDrawBlock;
-        last = -1;
-    }
-    __syncthreads();
-    before = start;
+    double x = 0.0, sum;
 #pragma unroll
-    for (int i = 0; i < kDrawLane / VEC; ++i) {
-        double x = 0.0;
+    for (int i = 0; i < kDrawLane; ++i) x += r.w[i];
+    double upto = (past ? 0.0 : before_picked) + block_scan(x, lds, sum) - x;
+    int first = kDrawBlock, end = -1;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) x += r.w[i * VEC + e];
-        double sum;
-        double upto = before + block_scan(x, lds, sum) - x;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-            const double w = r.w[i * VEC + e];
-            const int at = (i * kThreads + t) * VEC + e;
-            upto += w;
-            if (w > 0.0) {
-                atomicMax(&last, at);
-                if (!past && upto > goal) atomicMin(&picked, at);
-            }
+    for (int i = 0; i < kDrawLane; ++i) {
+        upto += r.w[i];
+        if (r.w[i] > 0.0) {
+            end = t * kDrawLane + i;
+            if (!past && upto > goal && first == kDrawBlock) first = end;
         }
-        before += sum;
     }
-    __syncthreads();
+    int picked, some;
+    first_and_last(first < kDrawBlock, first, end >= 0, end, kDrawBlock, lds_place, picked, some);
     if (t == 0) {
-        const int at = picked < kDrawBlock ? picked : last;
+        const int at = picked < kDrawBlock ? picked : some;
         a.following[b] = at < 0 ? -1 : (int64_t)seg * kDrawBlock + at;
     }
 }
@@ -651,7 +772,7 @@ hipError_t launch_type(const Verify &a, hipStream_t stream)
         else
             verify_sums_kernel<BF16, false><<<grid, kThreads, 0, stream>>>(a);
     }
-    verify_decide_kernel<<<(unsigned)a.n_seqs, 64, 0, stream>>>(a);
+    verify_decide_kernel<<<(unsigned)a.n_seqs, kThreads, 0, stream>>>(a);
     if (!greedy) {
         verify_weights_kernel<BF16>
             <<<(unsigned)(a.n_seqs * a.draw_segments), kThreads, 0, stream>>>(a);
@@ -661,6 +782,15 @@ hipError_t launch_type(const Verify &a, hipStream_t stream)
 }
 
 }  // namespace
+
+int64_t verify_segment(int64_t units, int64_t vocab)
+{
+    const int64_t blocks = (vocab + kSumBlock - 1) / kSumBlock;
+    int64_t n = units > 0 ? (16 * kServeCus + units - 1) / units : 1;
+    n = n > kVerifySegments ? kVerifySegments : n;
+    n = n > blocks ? blocks : n;
+    return (blocks + n - 1) / n * kSumBlock;
+}
 
 hipError_t launch_verify(const Verify &a, hipStream_t stream)
 {
