@@ -8,6 +8,7 @@
 
 #include "rrq_draft_launch.h"
 #include "rrq_serve_device.h"
+#include "rrq_wave.h"
 
 namespace rrq_detail {
 namespace {
@@ -86,8 +87,7 @@ __device__ __forceinline__ void store_piece(void *base, bool bf16, int64_t at, i
 // Sum over the workgroup. `lds` is this sum's own: no barrier guards it.
 __device__ __forceinline__ float block_sum(float a, float *lds)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) a += __shfl_xor(a, d);
+    a = wave_sum(a);
     const int waves = blockDim.x / 64;
     if (waves == 1) return a;
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = a;

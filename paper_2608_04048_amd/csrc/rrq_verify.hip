@@ -28,6 +28,7 @@
 
 #include "rrq_draft_launch.h"
 #include "rrq_serve_device.h"
+#include "rrq_wave.h"
 
 namespace rrq_detail {
 namespace {
@@ -136,50 +137,59 @@ __device__ __forceinline__ int place(int i)
     return RUNS ? (int)threadIdx.x * N + i : ((i / VEC) * kThreads + (int)threadIdx.x) * VEC + i % VEC;
 }
 
-// A thread's N logits of the block from `base` on. -inf past the vocabulary. Rows may
-// start at any multiple of their type.
+// A thread's N logits of the block from `base` on, as they are loaded: 16 bytes at a
+// time, without a branch between them. Rows may start at any multiple of their type; a
+// piece that passes the vocabulary's end is read from inside it and put right by unpack.
+struct __attribute__((packed, aligned(2))) Wide {
+    uint32_t w[4];
+};
 template <bool BF16, bool RUNS, int N>
-__device__ __forceinline__ void load_block(const void *row, int64_t base, int64_t vocab,
-                                           float (&v)[N])
-{
-    constexpr int VEC = BF16 ? 8 : 4, SIZE = BF16 ? 2 : 4;
-    struct __attribute__((packed, aligned(2))) Wide { uint32_t w[4]; };
-    const char *x = static_cast<const char *>(row);
-    const bool whole = base + (int64_t)kThreads * N <= vocab;
+struct Block {
+    static constexpr int VEC = BF16 ? 8 : 4, SIZE = BF16 ? 2 : 4;
+    Wide piece[N / VEC];
+
+    __device__ __forceinline__ void load(const void *row, int64_t base, int64_t vocab)
+    {
+        const char *x = static_cast<const char *>(row);
+        const bool whole = base + (int64_t)kThreads * N <= vocab;
+        if (!whole && vocab < VEC) return;
+        const int64_t end = vocab - VEC;
 #pragma unroll
-    for (int i = 0; i < N / VEC; ++i) {
-        const int64_t at = base + place<BF16, N, RUNS>(i * VEC);
-        if (whole || at + VEC <= vocab) {
-            const Wide w = *reinterpret_cast<const Wide *>(x + at * SIZE);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (BF16) {
-                    v[i * VEC + 2 * e] = __uint_as_float(w.w[e] << 16);
-                    v[i * VEC + 2 * e + 1] = __uint_as_float(w.w[e] & 0xFFFF0000u);
-                } else {
-                    v[i * VEC + e] = __uint_as_float(w.w[e]);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                v[i * VEC + e] = at + e < vocab ? logit(row, BF16, at + e) : -kInf;
+        for (int i = 0; i < N / VEC; ++i) {
+            const int64_t at = base + place<BF16, N, RUNS>(i * VEC);
+            piece[i] = *reinterpret_cast<const Wide *>(x + (whole || at < end ? at : end) * SIZE);
         }
     }
-}
+    // -inf past the vocabulary
+    __device__ __forceinline__ void unpack(const void *row, int64_t base, int64_t vocab,
+                                           float (&v)[N]) const
+    {
+#pragma unroll
+        for (int i = 0; i < N / VEC; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t w = piece[i].w[e];
+                if (BF16) {
+                    v[i * VEC + 2 * e] = __uint_as_float(w << 16);
+                    v[i * VEC + 2 * e + 1] = __uint_as_float(w & 0xFFFF0000u);
+                } else {
+                    v[i * VEC + e] = __uint_as_float(w);
+                }
+            }
+        if (base + (int64_t)kThreads * N <= vocab) return;
+#pragma unroll
+        for (int i = 0; i < N / VEC; ++i) {
+            const int64_t at = base + place<BF16, N, RUNS>(i * VEC);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) v[i * VEC + e] = at + e < vocab ? v[i * VEC + e] : -kInf;
+            if (at >= vocab || at + VEC <= vocab) continue;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)       // (of one thread)
+                if (at + e < vocab) v[i * VEC + e] = logit(row, BF16, at + e);
+        }
+    }
+};
 
-__device__ __forceinline__ float wave_max(float x)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) x = fmaxf(x, __shfl_xor(x, d));
-    return x;
-}
-__device__ __forceinline__ double wave_sum(double x)
-{
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
-    return x;
-}
 // Over the workgroup; lds: kWaves places, used by nothing else between two barriers.
 __device__ __forceinline__ float block_max(float x, float *lds)
 {
@@ -253,14 +263,15 @@ __global__ __launch_bounds__(kThreads) void verify_sums_kernel(Verify a)
     float m = -kInf;
     double sum = 0.0;
     int64_t best = a.vocab;
-    float v[kSumLane];
+    Block<BF16, false, kSumLane> block;
     int64_t base = (int64_t)seg * a.segment;
-    load_block<BF16, false>(row, base, a.vocab, v);
+    block.load(row, base, a.vocab);
     for (;;) {
+        float v[kSumLane];
+        block.unpack(row, base, a.vocab, v);
         // the next block is on its way under this one's sums
         const int64_t next = base + kSumBlock;
-        float w[kSumLane];
-        if (next < end) load_block<BF16, false>(row, next, a.vocab, w);
+        if (next < end) block.load(row, next, a.vocab);
         float bm = -kInf;
 #pragma unroll
         for (int i = 0; i < kSumLane; ++i) bm = fmaxf(bm, v[i]);
@@ -299,8 +310,6 @@ __global__ __launch_bounds__(kThreads) void verify_sums_kernel(Verify a)
         }
         if (next >= end) break;
         base = next;
-#pragma unroll
-        for (int i = 0; i < kSumLane; ++i) v[i] = w[i];
     }
     VerifySum *out = a.sums + unit * a.segments + seg;
     const float most = block_max(m, lds_max);
@@ -324,7 +333,7 @@ __global__ __launch_bounds__(kThreads) void verify_sums_kernel(Verify a)
 }
 
 // A row's largest logit and sum, from its segments, by kRowLanes neighbouring lanes.
-constexpr int kRowLanes = 16;
+constexpr int kRowLanes = 16;       // (a row of the wave)
 __device__ __forceinline__ void row_sum(const Verify &a, int64_t unit, double c, float &m,
                                         double &l)
 {
@@ -339,15 +348,13 @@ __device__ __forceinline__ void row_sum(const Verify &a, int64_t unit, double c,
         if (lane + k * kRowLanes < a.segments) x[k] = s[lane + k * kRowLanes];
         m = fmaxf(m, x[k].m);
     }
-#pragma unroll
-    for (int d = 1; d < kRowLanes; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+    m = row_max(m);
     l = 0.0;
 #pragma unroll
     for (int k = 0; k < kMost; ++k)
         l += x[k].m == -kInf ? x[k].sum
                              : x[k].sum * exp2_64(((double)x[k].m - (double)m) * c);
-#pragma unroll
-    for (int d = 1; d < kRowLanes; d *= 2) l += __shfl_xor(l, d);
+    l = row_total(l);
 }
 // A row's first largest logit, by as many lanes; the vocabulary's size for none.
 __device__ __forceinline__ int64_t row_best(const Verify &a, int64_t unit)
@@ -501,37 +508,21 @@ __global__ __launch_bounds__(kThreads) void verify_decide_kernel(Verify a)
     }
 }
 
-// Weights w of a thread's logits of block `seg` of the sequence's row, relative to the
-// logit m, and with a rejected draft the draft's, q. RUNS: as in place().
-struct Weights {
-    double w[kDrawLane], q[kDrawLane];
-};
+// A thread's logits v of block `seg` of the sequence's row, and with a rejected draft
+// the draft's, y. RUNS: as in place(). A token that was taken out is -inf.
 template <bool BF16, bool RUNS>
 __device__ __forceinline__ void load_logits(const Verify &a, int b, const VerifyChoice &c, int seg,
                                             float (&v)[kDrawLane], float (&y)[kDrawLane])
 {
-    load_block<BF16, RUNS>(target_row(a, c.row), (int64_t)seg * kDrawBlock, a.vocab, v);
-    if (c.draft >= 0)
-        load_block<BF16, RUNS>(draft_row(a, b, c.draft), (int64_t)seg * kDrawBlock, a.vocab, y);
-}
-template <bool BF16, bool RUNS>
-__device__ __forceinline__ void make_weights(const Verify &a, const VerifyChoice &c, int seg,
-                                             const float (&v)[kDrawLane],
-                                             const float (&y)[kDrawLane], float m,
-                                             const double *table, Weights &r)
-{
-    const float ms = m == -kInf ? 0.0f : m;
-    const double f = kTable * kLog2e * a.inv_temperature;
-#pragma unroll
-    for (int i = 0; i < kDrawLane; ++i) r.w[i] = weight(table, v[i], ms, f);
-    if (c.draft >= 0) {
-        const double fq = kTable * kLog2e * a.inv_draft_temperature;
-#pragma unroll
-        for (int i = 0; i < kDrawLane; ++i) r.q[i] = weight(table, y[i], c.mq, fq);
-    }
+    const int64_t base = (int64_t)seg * kDrawBlock;
+    const void *p = target_row(a, c.row), *q = draft_row(a, b, c.draft < 0 ? 0 : c.draft);
+    Block<BF16, RUNS, kDrawLane> x, z;
+    x.load(p, base, a.vocab);
+    if (c.draft >= 0) z.load(q, base, a.vocab);
+    x.unpack(p, base, a.vocab, v);
+    if (c.draft >= 0) z.unpack(q, base, a.vocab, y);
     if (!c.removed) return;
     // children of the row: 64 at a time, each wave on its own
-    const int64_t base = (int64_t)seg * kDrawBlock;
     const int lane = threadIdx.x & 63;
     for (int k0 = c.at + 1; k0 < c.n; k0 += 64) {
         const int k = k0 + lane;
@@ -544,10 +535,15 @@ __device__ __forceinline__ void make_weights(const Verify &a, const VerifyChoice
             const int at = (int)(__shfl(token, i) - base);
 #pragma unroll
             for (int e = 0; e < kDrawLane; ++e)
-                if (at == place<BF16, kDrawLane, RUNS>(e)) r.w[e] = 0.0;
+                if (at == place<BF16, kDrawLane, RUNS>(e)) v[e] = -kInf;
         }
         if (!a.parents) break;      // a chain's row has one child, the next
     }
+}
+// Factors of weight() for the target's logits and the draft's.
+__device__ __forceinline__ double weight_factor(double inv_temperature)
+{
+    return kTable * kLog2e * inv_temperature;
 }
 
 // Step 3: one workgroup a block of the vocabulary.
@@ -570,23 +566,27 @@ __global__ __launch_bounds__(kThreads) void verify_weights_kernel(Verify a)
         for (int i = 0; i < kDrawLane; ++i) m = fmaxf(m, v[i]);
         m = block_max(m, lds_max);
     }
-    Weights r;
-    make_weights<BF16, false>(a, c, seg, v, y, m, table, r);
+    const float ms = m == -kInf ? 0.0f : m;
+    const double f = weight_factor(a.inv_temperature);
     double p = 0.0, q = 0.0, sp = 0.0, sq = 0.0;
-#pragma unroll
-    for (int i = 0; i < kDrawLane; ++i) p += r.w[i];
     if (c.draft >= 0) {
+        const double fq = weight_factor(a.inv_draft_temperature);
 #pragma unroll
         for (int i = 0; i < kDrawLane; ++i) {
-            q += r.q[i];
-            if (r.w[i] * c.lq > r.q[i] * c.l) {
-                sp += r.w[i];
-                sq += r.q[i];
+            const double w = weight(table, v[i], ms, f), x = weight(table, y[i], c.mq, fq);
+            p += w;
+            q += x;
+            if (w * c.lq > x * c.l) {
+                sp += w;
+                sq += x;
             }
         }
         q = wave_sum(q);
         sp = wave_sum(sp);
         sq = wave_sum(sq);
+    } else {
+#pragma unroll
+        for (int i = 0; i < kDrawLane; ++i) p += weight(table, v[i], ms, f);
     }
     p = wave_sum(p);
     if ((threadIdx.x & 63) == 0) {
@@ -613,11 +613,7 @@ __global__ __launch_bounds__(kThreads) void verify_weights_kernel(Verify a)
 __device__ __forceinline__ double block_scan(double x, double *lds, double &total)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const double y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
+    x = wave_scan(x);
     __syncthreads();
     if (lane == 63) lds[wave] = x;
     __syncthreads();
@@ -732,22 +728,29 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(Verify a)
     }
     float v[kDrawLane], y[kDrawLane];
     load_logits<BF16, true>(a, b, c, seg, v, y);
-    Weights r;
-    make_weights<BF16, true>(a, c, seg, v, y, m, table, r);
-    if (residual) {
+    const float ms = m == -kInf ? 0.0f : m;
+    double w[kDrawLane];
+    {
+        const double fp = weight_factor(a.inv_temperature);
+        const double fq = weight_factor(a.inv_draft_temperature);
 #pragma unroll
-        for (int i = 0; i < kDrawLane; ++i)
-            r.w[i] = r.w[i] * c.lq > r.q[i] * c.l ? fmax(r.w[i] / lp - r.q[i] / lq, 0.0) : 0.0;
+        for (int i = 0; i < kDrawLane; ++i) {
+            w[i] = weight(table, v[i], ms, fp);
+            if (residual) {
+                const double q = weight(table, y[i], c.mq, fq);
+                w[i] = w[i] * c.lq > q * c.l ? fmax(w[i] / lp - q / lq, 0.0) : 0.0;
+            }
+        }
     }
     double x = 0.0, sum;
 #pragma unroll
-    for (int i = 0; i < kDrawLane; ++i) x += r.w[i];
+    for (int i = 0; i < kDrawLane; ++i) x += w[i];
     double upto = (past ? 0.0 : before_picked) + block_scan(x, lds, sum) - x;
     int first = kDrawBlock, end = -1;
 #pragma unroll
     for (int i = 0; i < kDrawLane; ++i) {
-        upto += r.w[i];
-        if (r.w[i] > 0.0) {
+        upto += w[i];
+        if (w[i] > 0.0) {
             end = t * kDrawLane + i;
             if (!past && upto > goal && first == kDrawBlock) first = end;
         }
