@@ -35,10 +35,13 @@ namespace {
 
 constexpr float kInf = __builtin_inff();
 constexpr double kLn2 = 0.69314718055994530942, kLog2e = 1.44269504088896340736;
-constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kSumLane = 32, kSumBlock = kThreads * kSumLane;       // logits of step 1
-constexpr int kDrawLane = 16, kDrawBlock = kThreads * kDrawLane;    // of steps 3 and 4
-static_assert(kSumBlock == kVerifySumBlock && kDrawBlock == kVerifyDrawBlock, "workspace");
+constexpr int kThreads = 256;
+// Logits a thread takes: in step 1; in step 3, and in step 4, whose one workgroup a
+// sequence has twice the threads, as its time is a single wave's.
+constexpr int kSumLane = 32, kWeightLane = 16, kDrawLane = 8, kDrawThreads = 512;
+constexpr int kSumBlock = kThreads * kSumLane, kDrawBlock = kThreads * kWeightLane;
+static_assert(kSumBlock == kVerifySumBlock && kDrawBlock == kVerifyDrawBlock &&
+                  kDrawBlock == kDrawThreads * kDrawLane, "blocks of the workspace");
 
 // 2^y, y of any size; a NaN stays one.
 __device__ __forceinline__ double exp2_64(double y)
@@ -66,16 +69,17 @@ __device__ __forceinline__ double weight(float x, float m, double c)
     return exp2_64(((double)x - (double)m) * c);
 }
 
-// The same from a table of 2^(i / 32) in LDS (no two of which share a bank) and a
-// series of degree 5: half the instructions of the whole one.
-constexpr int kTable = 32;
+// The same from a table of 2^(i / 256) in LDS and a series of degree 3 (2e-13): half
+// the instructions of the whole one. (32 entries, no two of which share a bank, and
+// degree 5: two instructions of 20 more.)
+constexpr int kTable = 256;
 __device__ __forceinline__ void fill_table(double *table)
 {
     if (threadIdx.x < kTable) table[threadIdx.x] = exp2_64(threadIdx.x * (1.0 / kTable));
     __syncthreads();
 }
-// c: 32 log2(e) / T. The sum with 1.5 2^52 rounds y to a whole number, which its low
-// bits are.
+// c: kTable log2(e) / T. The sum with 1.5 2^52 rounds y to a whole number, which its
+// low bits are.
 __device__ __forceinline__ double weight(const double *table, float x, float m, double c)
 {
     constexpr double kRound = 6755399441055744.0, L = kLn2 / kTable;
@@ -83,13 +87,10 @@ __device__ __forceinline__ double weight(const double *table, float x, float m, 
     const double t = y + kRound;
     const int n = (int)(uint32_t)__builtin_bit_cast(uint64_t, t);
     const double r = y - (t - kRound);
-    double p = L * L * L * L * L / 120.0;
-    p = __builtin_fma(p, r, L * L * L * L / 24.0);
-    p = __builtin_fma(p, r, L * L * L / 6.0);
-    p = __builtin_fma(p, r, L * L / 2.0);
+    double p = __builtin_fma(L * L * L / 6.0, r, L * L / 2.0);
     p = __builtin_fma(p, r, L);
     p = __builtin_fma(p, r, 1.0);
-    p = __builtin_amdgcn_ldexp(table[n & (kTable - 1)] * p, n >> 5);
+    p = __builtin_amdgcn_ldexp(table[n & (kTable - 1)] * p, n >> 8);
     return y < -1000.0 * kTable ? 0.0 : p;
 }
 
@@ -128,13 +129,13 @@ __device__ __forceinline__ const void *draft_row(const Verify &a, int64_t b, int
            (b * a.draft_seq_stride + j * a.draft_row_stride) * (a.bf16 ? 2 : 4);
 }
 
-// Where in a block of kThreads * N logits a thread's i-th stands: VEC (16 bytes) in a
+// Where in a block of T threads' N logits a thread's i-th stands: VEC (16 bytes) in a
 // row; RUNS: N in a row.
-template <bool BF16, int N, bool RUNS>
+template <bool BF16, int N, bool RUNS, int T>
 __device__ __forceinline__ int place(int i)
 {
     constexpr int VEC = BF16 ? 8 : 4;
-    return RUNS ? (int)threadIdx.x * N + i : ((i / VEC) * kThreads + (int)threadIdx.x) * VEC + i % VEC;
+    return RUNS ? (int)threadIdx.x * N + i : ((i / VEC) * T + (int)threadIdx.x) * VEC + i % VEC;
 }
 
 // A thread's N logits of the block from `base` on, as they are loaded: 16 bytes at a
@@ -143,7 +144,7 @@ __device__ __forceinline__ int place(int i)
 struct __attribute__((packed, aligned(2))) Wide {
     uint32_t w[4];
 };
-template <bool BF16, bool RUNS, int N>
+template <bool BF16, bool RUNS, int N, int T>
 struct Block {
     static constexpr int VEC = BF16 ? 8 : 4, SIZE = BF16 ? 2 : 4;
     Wide piece[N / VEC];
@@ -151,12 +152,12 @@ struct Block {
     __device__ __forceinline__ void load(const void *row, int64_t base, int64_t vocab)
     {
         const char *x = static_cast<const char *>(row);
-        const bool whole = base + (int64_t)kThreads * N <= vocab;
+        const bool whole = base + (int64_t)T * N <= vocab;
         if (!whole && vocab < VEC) return;
         const int64_t end = vocab - VEC;
 #pragma unroll
         for (int i = 0; i < N / VEC; ++i) {
-            const int64_t at = base + place<BF16, N, RUNS>(i * VEC);
+            const int64_t at = base + place<BF16, N, RUNS, T>(i * VEC);
             piece[i] = *reinterpret_cast<const Wide *>(x + (whole || at < end ? at : end) * SIZE);
         }
     }
@@ -176,10 +177,10 @@ struct Block {
                     v[i * VEC + e] = __uint_as_float(w);
                 }
             }
-        if (base + (int64_t)kThreads * N <= vocab) return;
+        if (base + (int64_t)T * N <= vocab) return;
 #pragma unroll
         for (int i = 0; i < N / VEC; ++i) {
-            const int64_t at = base + place<BF16, N, RUNS>(i * VEC);
+            const int64_t at = base + place<BF16, N, RUNS, T>(i * VEC);
 #pragma unroll
             for (int e = 0; e < VEC; ++e) v[i * VEC + e] = at + e < vocab ? v[i * VEC + e] : -kInf;
             if (at >= vocab || at + VEC <= vocab) continue;
@@ -190,8 +191,9 @@ struct Block {
     }
 };
 
-// Over the workgroup; lds: kWaves places, used by nothing else between two barriers.
-__device__ __forceinline__ float block_max(float x, float *lds)
+// Over a workgroup of W waves; lds is used by nothing else between two barriers.
+template <int W>
+__device__ __forceinline__ float block_max(float x, float (&lds)[W])
 {
     x = wave_max(x);
     __syncthreads();
@@ -199,10 +201,11 @@ __device__ __forceinline__ float block_max(float x, float *lds)
     __syncthreads();
     x = lds[0];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) x = fmaxf(x, lds[w]);
+    for (int w = 1; w < W; ++w) x = fmaxf(x, lds[w]);
     return x;
 }
-__device__ __forceinline__ double block_sum(double x, double *lds)
+template <int W>
+__device__ __forceinline__ double block_sum(double x, double (&lds)[W])
 {
     x = wave_sum(x);
     __syncthreads();
@@ -210,7 +213,7 @@ __device__ __forceinline__ double block_sum(double x, double *lds)
     __syncthreads();
     x = lds[0];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) x += lds[w];
+    for (int w = 1; w < W; ++w) x += lds[w];
     return x;
 }
 
@@ -228,8 +231,9 @@ __device__ __forceinline__ bool has_child(const Verify &a, int o0, int n, int j)
 template <bool BF16, bool GREEDY>
 __global__ __launch_bounds__(kThreads) void verify_sums_kernel(Verify a)
 {
-    __shared__ float lds_max[kWaves];
-    __shared__ double lds_sum[kWaves];
+    constexpr int W = kThreads / 64;
+    __shared__ float lds_max[W];
+    __shared__ double lds_sum[W];
     const int64_t unit = blockIdx.x / (uint32_t)a.segments;
     const int seg = blockIdx.x % (uint32_t)a.segments;
     const void *row;
@@ -263,7 +267,7 @@ __global__ __launch_bounds__(kThreads) void verify_sums_kernel(Verify a)
     float m = -kInf;
     double sum = 0.0;
     int64_t best = a.vocab;
-    Block<BF16, false, kSumLane> block;
+    Block<BF16, false, kSumLane, kThreads> block;
     int64_t base = (int64_t)seg * a.segment;
     block.load(row, base, a.vocab);
     for (;;) {
@@ -272,41 +276,63 @@ __global__ __launch_bounds__(kThreads) void verify_sums_kernel(Verify a)
         // the next block is on its way under this one's sums
         const int64_t next = base + kSumBlock;
         if (next < end) block.load(row, next, a.vocab);
-        float bm = -kInf;
+        auto largest = [&] {
+            float x = v[0] == v[0] ? v[0] : -kInf;
 #pragma unroll
-        for (int i = 0; i < kSumLane; ++i) bm = fmaxf(bm, v[i]);
+            for (int i = 1; i < kSumLane; ++i) x = fmaxf(x, v[i]);
+            return x;
+        };
         if (GREEDY) {
             // the first place of a thread's largest (blocks ascend)
+            const float bm = largest();
             if (bm > m || best == a.vocab) {
 #pragma unroll
                 for (int i = kSumLane - 1; i >= 0; --i) {
-                    const int64_t at = base + place<BF16, kSumLane, false>(i);
+                    const int64_t at = base + place<BF16, kSumLane, false, kThreads>(i);
                     if (v[i] == bm && at < a.vocab) best = at;
                 }
                 m = bm;
             }
         } else {
-            // a thread's sum is relative to its own largest
-            if (bm > m) {
-                sum *= m == -kInf ? 0.0 : exp2_64(((double)m - (double)bm) * c);
-                m = bm;
-            }
-            const float ms = m == -kInf ? 0.0f : m;
-            float t = 0.0f;
-            double s = 0.0;
+            // s = sum w, t = sum w d, w = e^(d / T), d relative to m
+            double s;
+            float t;
+            auto add = [&](auto cut) {
+                s = 0.0;
+                t = 0.0f;
 #pragma unroll
-            for (int i = 0; i < kSumLane; i += 8) {
-                float part = 0.0f;
+                for (int i = 0; i < kSumLane; i += 8) {
+                    float part = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float d = v[i + e] - ms, x = __builtin_amdgcn_exp2f(d * ch);
-                    part += x;
-                    // (-inf times 0 is kept out)
-                    t = __builtin_fmaf(x, fmaxf(d, -1e30f), t);
+                    for (int e = 0; e < 8; ++e) {
+                        const float d = v[i + e] - m, x = __builtin_amdgcn_exp2f(d * ch);
+                        part += x;
+                        t = __builtin_fmaf(x, cut(d), t);
+                    }
+                    s += (double)part;
                 }
-                s += (double)part;
+            };
+            // A thread's m is the largest logit of its first block that has any: later
+            // ones need no maximum of their own until a sum says that they do.
+            if (m == -kInf) m = largest();
+            if (m > -kInf) {
+                add([](float d) { return d; });
+                const bool far = !(s < 0x1p60);
+                // (a logit of -inf makes t no number; so may one that is none)
+                if (far || t != t) {
+                    if (far) {
+                        const float more = fmaxf(m, largest());
+                        sum *= exp2_64(((double)m - (double)more) * c);
+                        m = more;
+                    }
+                    add([](float d) { return fmaxf(d, -1e30f); });
+                }
+                sum += s + kLn2 * cl * (double)t;
+            } else {
+                // nothing but -inf and what is no number
+#pragma unroll
+                for (int i = 0; i < kSumLane; ++i) sum += v[i] == v[i] ? 0.0 : (double)v[i];
             }
-            sum += s + kLn2 * cl * (double)t;
         }
         if (next >= end) break;
         base = next;
@@ -322,7 +348,7 @@ __global__ __launch_bounds__(kThreads) void verify_sums_kernel(Verify a)
         __syncthreads();
         if (threadIdx.x == 0) {
 #pragma unroll
-            for (int w = 1; w < kWaves; ++w) at = fmin(at, lds_sum[w]);
+            for (int w = 1; w < W; ++w) at = fmin(at, lds_sum[w]);
             *out = VerifySum{most, 0, at};
         }
         return;
@@ -389,7 +415,8 @@ __device__ __forceinline__ double lane_value(double x, int i)
 
 // Step 2: one workgroup a sequence. Of 64 rows at a time, kRowLanes lanes a row find
 // the token's probability under its parent; the first wave walks.
-__global__ __launch_bounds__(kThreads) void verify_decide_kernel(Verify a)
+constexpr int kDecideThreads = 64 * kRowLanes;
+__global__ __launch_bounds__(kDecideThreads) void verify_decide_kernel(Verify a)
 {
     struct Row {
         double w, q, l, lq;
@@ -402,14 +429,14 @@ __global__ __launch_bounds__(kThreads) void verify_decide_kernel(Verify a)
     int n;
     const int o0 = rows_of(a, b, n);
     int32_t *path = a.paths + (int64_t)b * (a.max_accept + 1);
-    for (int i = t; i <= a.max_accept; i += kThreads) path[i] = i == 0 && n > 0 ? 0 : -1;
+    for (int i = t; i <= a.max_accept; i += kDecideThreads) path[i] = i == 0 && n > 0 ? 0 : -1;
     const double c = kLog2e * a.inv_temperature, cq = kLog2e * a.inv_draft_temperature;
     int at = 0, count = 0, rejected = -1;
     double mass = 1.0;
     for (int base = 0; base < n && count < a.max_accept && rejected < 0; base += 64) {
-        for (int k = t / kRowLanes; k < 64 && base + k < n; k += kThreads / kRowLanes) {
-            const int j = base + k, parent = parent_of(a, o0, j);
-            if (parent < 0) continue;
+        const int k = t / kRowLanes;
+        if (const int parent = base + k < n ? parent_of(a, o0, base + k) : -1; parent >= 0) {
+            const int j = base + k;
             const int64_t token = a.tokens[o0 + j];
             const bool inside = token >= 0 && token < a.vocab;
             Row r = {};
@@ -510,13 +537,14 @@ __global__ __launch_bounds__(kThreads) void verify_decide_kernel(Verify a)
 
 // A thread's logits v of block `seg` of the sequence's row, and with a rejected draft
 // the draft's, y. RUNS: as in place(). A token that was taken out is -inf.
-template <bool BF16, bool RUNS>
+template <bool BF16, bool RUNS, int T, int N>
 __device__ __forceinline__ void load_logits(const Verify &a, int b, const VerifyChoice &c, int seg,
-                                            float (&v)[kDrawLane], float (&y)[kDrawLane])
+                                            float (&v)[N], float (&y)[N])
 {
+    static_assert(T * N == kDrawBlock, "a block");
     const int64_t base = (int64_t)seg * kDrawBlock;
     const void *p = target_row(a, c.row), *q = draft_row(a, b, c.draft < 0 ? 0 : c.draft);
-    Block<BF16, RUNS, kDrawLane> x, z;
+    Block<BF16, RUNS, N, T> x, z;
     x.load(p, base, a.vocab);
     if (c.draft >= 0) z.load(q, base, a.vocab);
     x.unpack(p, base, a.vocab, v);
@@ -534,8 +562,8 @@ __device__ __forceinline__ void load_logits(const Verify &a, int b, const Verify
             here &= here - 1;
             const int at = (int)(__shfl(token, i) - base);
 #pragma unroll
-            for (int e = 0; e < kDrawLane; ++e)
-                if (at == place<BF16, kDrawLane, RUNS>(e)) v[e] = -kInf;
+            for (int e = 0; e < N; ++e)
+                if (at == place<BF16, N, RUNS, T>(e)) v[e] = -kInf;
         }
         if (!a.parents) break;      // a chain's row has one child, the next
     }
@@ -550,20 +578,21 @@ __device__ __forceinline__ double weight_factor(double inv_temperature)
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void verify_weights_kernel(Verify a)
 {
-    __shared__ float lds_max[kWaves];
-    __shared__ double lds[4][kWaves], table[kTable];
+    constexpr int W = kThreads / 64;
+    __shared__ float lds_max[W];
+    __shared__ double lds[4][W], table[kTable];
     const int b = blockIdx.x / (uint32_t)a.draw_segments;
     const int seg = blockIdx.x % (uint32_t)a.draw_segments;
     const VerifyChoice c = a.choices[b];
     if (c.row < 0) return;
-    float v[kDrawLane], y[kDrawLane];
-    load_logits<BF16, false>(a, b, c, seg, v, y);
+    float v[kWeightLane], y[kWeightLane];
+    load_logits<BF16, false, kThreads>(a, b, c, seg, v, y);
     fill_table(table);
     float m = c.m;
     if (c.draft < 0) {
         m = -kInf;
 #pragma unroll
-        for (int i = 0; i < kDrawLane; ++i) m = fmaxf(m, v[i]);
+        for (int i = 0; i < kWeightLane; ++i) m = fmaxf(m, v[i]);
         m = block_max(m, lds_max);
     }
     const float ms = m == -kInf ? 0.0f : m;
@@ -572,7 +601,7 @@ __global__ __launch_bounds__(kThreads) void verify_weights_kernel(Verify a)
     if (c.draft >= 0) {
         const double fq = weight_factor(a.inv_draft_temperature);
 #pragma unroll
-        for (int i = 0; i < kDrawLane; ++i) {
+        for (int i = 0; i < kWeightLane; ++i) {
             const double w = weight(table, v[i], ms, f), x = weight(table, y[i], c.mq, fq);
             p += w;
             q += x;
@@ -586,7 +615,7 @@ __global__ __launch_bounds__(kThreads) void verify_weights_kernel(Verify a)
         sq = wave_sum(sq);
     } else {
 #pragma unroll
-        for (int i = 0; i < kDrawLane; ++i) p += weight(table, v[i], ms, f);
+        for (int i = 0; i < kWeightLane; ++i) p += weight(table, v[i], ms, f);
     }
     p = wave_sum(p);
     if ((threadIdx.x & 63) == 0) {
@@ -603,14 +632,15 @@ __global__ __launch_bounds__(kThreads) void verify_weights_kernel(Verify a)
     for (int i = 0; i < 4; ++i) {
         all[i] = lds[i][0];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) all[i] += lds[i][w];
+        for (int w = 1; w < W; ++w) all[i] += lds[i][w];
     }
     a.blocks[(int64_t)b * a.draw_segments + seg] =
         VerifyBlock{all[0], all[1], all[2], all[3], m, 0};
 }
 
 // Inclusive sum over the workgroup's threads; total: of all.
-__device__ __forceinline__ double block_scan(double x, double *lds, double &total)
+template <int W>
+__device__ __forceinline__ double block_scan(double x, double (&lds)[W], double &total)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     x = wave_scan(x);
@@ -620,7 +650,7 @@ __device__ __forceinline__ double block_scan(double x, double *lds, double &tota
     double before = 0.0;
     total = 0.0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
         if (w < wave) before += lds[w];
         total += lds[w];
     }
@@ -629,8 +659,9 @@ __device__ __forceinline__ double block_scan(double x, double *lds, double &tota
 
 // The first thread that has `is`, of it `at`, and the last that has `was`, of it `to`;
 // `none` and -1 for none. Places ascend with threads.
+template <int W>
 __device__ __forceinline__ void first_and_last(bool is, int at, bool was, int to, int none,
-                                               int (*lds)[kWaves], int &first, int &last)
+                                               int (&lds)[2][W], int &first, int &last)
 {
     const int wave = threadIdx.x >> 6;
     const uint64_t i = __ballot(is), w = __ballot(was);
@@ -645,7 +676,7 @@ __device__ __forceinline__ void first_and_last(bool is, int at, bool was, int to
     first = none;
     last = -1;
 #pragma unroll
-    for (int k = 0; k < kWaves; ++k) {
+    for (int k = 0; k < W; ++k) {
         first = lds[0][k] < first ? lds[0][k] : first;
         last = lds[1][k] > last ? lds[1][k] : last;
     }
@@ -653,31 +684,33 @@ __device__ __forceinline__ void first_and_last(bool is, int at, bool was, int to
 
 // Step 4: one workgroup a sequence.
 template <bool BF16>
-__global__ __launch_bounds__(kThreads) void verify_draw_kernel(Verify a)
+__global__ __launch_bounds__(kDrawThreads) void verify_draw_kernel(Verify a)
 {
-    __shared__ float lds_max[kWaves];
-    __shared__ double lds[kWaves], table[kTable];
-    __shared__ int lds_place[2][kWaves];
+    constexpr int W = kDrawThreads / 64;
+    __shared__ float lds_max[W];
+    __shared__ double lds[W], table[kTable];
+    __shared__ int lds_place[2][W];
     __shared__ double before_picked;
     const int b = blockIdx.x, t = threadIdx.x;
     const VerifyChoice c = a.choices[b];
     if (c.row < 0) return;
     const VerifyBlock *blocks = a.blocks + (int64_t)b * a.draw_segments;
     const double f = kLog2e * a.inv_temperature;
+    const double u = (double)a.uniforms[c.first];
     // this thread's block of the first round, read once
     VerifyBlock mine = {0.0, 0.0, 0.0, 0.0, -kInf, 0};
     if (t < a.draw_segments) mine = blocks[t];
     fill_table(table);
-    auto block = [&](int i) { return i < kThreads ? mine : blocks[i]; };
+    auto block = [&](int i) { return i < kDrawThreads ? mine : blocks[i]; };
     float m = mine.m;
-    for (int i = t + kThreads; i < a.draw_segments; i += kThreads) m = fmaxf(m, blocks[i].m);
+    for (int i = t + kDrawThreads; i < a.draw_segments; i += kDrawThreads) m = fmaxf(m, blocks[i].m);
     m = block_max(m, lds_max);
     // a block's weights relative to the row's largest logit
     auto whole = [&](const VerifyBlock &k) {
         return k.m == -kInf ? k.p : k.p * exp2_64(((double)k.m - (double)m) * f);
     };
     double lp = 0.0, lq = 0.0, res = 0.0;
-    for (int i = t; i < a.draw_segments; i += kThreads) {
+    for (int i = t; i < a.draw_segments; i += kDrawThreads) {
         const VerifyBlock k = block(i);
         lp += whole(k);
         lq += k.q;
@@ -686,7 +719,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(Verify a)
     bool residual = c.draft >= 0;
     if (residual) {
         lq = block_sum(lq, lds);
-        for (int i = t; i < a.draw_segments; i += kThreads) {
+        for (int i = t; i < a.draw_segments; i += kDrawThreads) {
             const VerifyBlock k = block(i);
             res += fmax(k.sp / lp - k.sq / lq, 0.0);
         }
@@ -698,11 +731,11 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(Verify a)
         if (t == 0) a.following[b] = -1;
         return;
     }
-    const double goal = (double)a.uniforms[c.first] * total;
+    const double goal = u * total;
     // the first block past which the sum exceeds the goal, the last that has any
     int seg = a.draw_segments, last = -1;
     double before = 0.0;
-    for (int i0 = 0; i0 < a.draw_segments && seg == a.draw_segments; i0 += kThreads) {
+    for (int i0 = 0; i0 < a.draw_segments && seg == a.draw_segments; i0 += kDrawThreads) {
         const int i = i0 + t;
         double x = 0.0;
         if (i < a.draw_segments) {
@@ -727,7 +760,7 @@ __global__ __launch_bounds__(kThreads) void verify_draw_kernel(Verify a)
         return;
     }
     float v[kDrawLane], y[kDrawLane];
-    load_logits<BF16, true>(a, b, c, seg, v, y);
+    load_logits<BF16, true, kDrawThreads>(a, b, c, seg, v, y);
     const float ms = m == -kInf ? 0.0f : m;
     double w[kDrawLane];
     {
@@ -775,11 +808,11 @@ hipError_t launch_type(const Verify &a, hipStream_t stream)
         else
             verify_sums_kernel<BF16, false><<<grid, kThreads, 0, stream>>>(a);
     }
-    verify_decide_kernel<<<(unsigned)a.n_seqs, kThreads, 0, stream>>>(a);
+    verify_decide_kernel<<<(unsigned)a.n_seqs, kDecideThreads, 0, stream>>>(a);
     if (!greedy) {
         verify_weights_kernel<BF16>
             <<<(unsigned)(a.n_seqs * a.draw_segments), kThreads, 0, stream>>>(a);
-        verify_draw_kernel<BF16><<<(unsigned)a.n_seqs, kThreads, 0, stream>>>(a);
+        verify_draw_kernel<BF16><<<(unsigned)a.n_seqs, kDrawThreads, 0, stream>>>(a);
     }
     return hipGetLastError();
 }
