@@ -477,7 +477,8 @@ hipError_t join_dim(const Attend &a, hipStream_t stream)
 
 }  // namespace
 
-AttendPlan attend_plan(const rrq_cache &c, const rrq_batch &b, int n_heads, int64_t window)
+AttendPlan attend_plan(const rrq_cache &c, const rrq_batch &b, int n_heads, int64_t window,
+                       bool tree)
 {
     const int ratio = n_heads / c.n_kv_heads;
     AttendPlan p = {};
@@ -498,6 +499,24 @@ AttendPlan attend_plan(const rrq_cache &c, const rrq_batch &b, int n_heads, int6
     p.rows_form = rows > (c.head_dim == 64 ? 64 : 32) * b.n_seqs &&
                   attend_row_tiles(b, ratio, p.tile) * c.n_kv_heads > kServeCus / 4;
     if (p.rows_form) p.tile = kRowsTile;
+    // Drafted tokens of few sequences: as long as all pairs of a 16-row tile and a tile
+    // of keys are few, time is the latency of a range, and shortest in 16-row tiles.
+    // Heads of 128: 25 rows x 4 on 2000 positions (1700 pairs) 15.2 us in tiles of 16
+    // and 17.7 in tiles of 32, 60 x 4 on 3000 (6000) 24.8 and 26.0, 25 x 4 on 8000
+    // (7000) 31 and 27. Heads of 256, 9 to 17 x 4 of 6 sequences: in a window of 1024
+    // (2000) 23.2 and in the many-row form 33.6, on 7000 (11900) 60 and 69; of 16
+    // sequences (30000) 113 and 79. Heads of 64, 8 sequences of 12 x 12 on 5000 (10000)
+    // 22.5 and 25.1.
+    if (tree) {
+        int64_t keys = b.max_pages * c.page_size;
+        if (window > 0 && window < keys) keys = window;
+        const int64_t pairs = attend_row_tiles(b, ratio, 16) * c.n_kv_heads *
+                              ((keys + kTileKeys - 1) / kTileKeys);
+        if (pairs <= (c.head_dim == 128 ? 6400 : 12800)) {
+            p.tile = 16;
+            p.rows_form = false;
+        }
+    }
     const int64_t units = attend_row_tiles(b, ratio, p.tile) * c.n_kv_heads;
     p.lds_rows = rows < 16 ? (int)rows : 16;
     p.waves = 4;

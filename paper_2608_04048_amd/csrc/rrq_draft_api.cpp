@@ -132,7 +132,7 @@ extern "C" int rrq_tree_attention(const rrq_cache *cache, const rrq_batch *batch
     AttendPlan plan = {};
     const AttendCall call = {Q, out, workspace, q_token_stride, q_head_stride, window,
                              workspace_bytes, scale, q_dtype, out_dtype, n_heads, 0};
-    const int st = prepare_attend(cache, batch, call, a, plan);
+    const int st = prepare_attend(cache, batch, call, a, plan, true);
     if (st != RRQ_OK) return st;
     if (seen_words < 1 || seen_words > (int64_t(1) << 20)) return RRQ_ERR_SHAPE;
     if (plan.splits == 0) return RRQ_OK;

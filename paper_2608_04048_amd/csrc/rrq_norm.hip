@@ -138,7 +138,16 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(BlockNorm a)
     auto first = [&](int c) { return kPiece * (int)(c * blockDim.x + threadIdx.x); };
     auto n_of = [&](int c) { return N - first(c); };    // (more than kPiece: a whole piece)
 
-    float h[CH][kPiece], y[CH][kPiece];
+    // What a row of few pieces needs is on its way before the first sum; longer rows
+    // would not have the registers.
+    constexpr bool kAhead = CH <= 2;
+    float h[CH][kPiece], y[CH][kPiece], g[CH][kPiece], w[CH][kPiece], p[CH][kPiece];
+    const bool post = a.norm.post != RRQ_NORM_NONE;
+    auto load_post = [&](int c) { load_piece<false>(a.norm.post_weight, first(c), n_of(c), p[c]); };
+    auto load_gate = [&](int c) {
+        load_piece<Y16>(a.gate, row * a.gate_stride + first(c), n_of(c), g[c]);
+    };
+    auto load_weight = [&](int c) { load_piece<false>(a.norm.weight, first(c), n_of(c), w[c]); };
     if (a.y) {
 #pragma unroll
         for (int c = 0; c < CH; ++c)
@@ -147,26 +156,32 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(BlockNorm a)
 #pragma unroll
     for (int c = 0; c < CH; ++c)
         load_piece<R16>(a.residual, row * a.r_stride + first(c), n_of(c), h[c]);
+    if (kAhead) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            if (a.gate) load_gate(c);
+            if (a.norm.post_weight) load_post(c);
+            if (a.norm.weight) load_weight(c);
+        }
+    }
     if (a.y) {
-        if (a.norm.post != RRQ_NORM_NONE) {
+        if (post) {
             normalise(y, a.norm.post, inv_n, a.norm.eps, lds, n_of);
             if (a.norm.post_weight) {
 #pragma unroll
                 for (int c = 0; c < CH; ++c) {
-                    float w[kPiece];
-                    load_piece<false>(a.norm.post_weight, first(c), n_of(c), w);
+                    if (!kAhead) load_post(c);
 #pragma unroll
-                    for (int e = 0; e < kPiece; ++e) y[c][e] *= w[e];
+                    for (int e = 0; e < kPiece; ++e) y[c][e] *= p[c][e];
                 }
             }
         }
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             if (a.gate) {
-                float g[kPiece];
-                load_piece<Y16>(a.gate, row * a.gate_stride + first(c), n_of(c), g);
+                if (!kAhead) load_gate(c);
 #pragma unroll
-                for (int e = 0; e < kPiece; ++e) y[c][e] *= g[e];
+                for (int e = 0; e < kPiece; ++e) y[c][e] *= g[c][e];
             }
 #pragma unroll
             for (int e = 0; e < kPiece; ++e) h[c][e] += y[c][e] * a.norm.scale;
@@ -177,16 +192,14 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(BlockNorm a)
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         if (a.norm.weight) {
-            float w[kPiece];
-            load_piece<false>(a.norm.weight, first(c), n_of(c), w);
+            if (!kAhead) load_weight(c);
 #pragma unroll
-            for (int e = 0; e < kPiece; ++e) h[c][e] *= w[e];
+            for (int e = 0; e < kPiece; ++e) h[c][e] *= w[c][e];
         }
         if (a.norm.bias) {
-            float w[kPiece];
-            load_piece<false>(a.norm.bias, first(c), n_of(c), w);
+            load_piece<false>(a.norm.bias, first(c), n_of(c), w[c]);
 #pragma unroll
-            for (int e = 0; e < kPiece; ++e) h[c][e] += w[e];
+            for (int e = 0; e < kPiece; ++e) h[c][e] += w[c][e];
         }
         store_piece(a.out, a.out_bf16, row * N + first(c), n_of(c), h[c]);
     }

@@ -92,7 +92,7 @@ struct AttendCall {
 // Checks a call's arguments and fills in what the launch takes. plan.splits stays 0
 // for a call that has nothing to do.
 inline int prepare_attend(const rrq_cache *cache, const rrq_batch *batch, const AttendCall &c,
-                          Attend &a, AttendPlan &plan)
+                          Attend &a, AttendPlan &plan, bool tree = false)
 {
     int st = check_cache(cache, true);
     if (st == RRQ_OK) st = check_batch(batch, true);
@@ -119,7 +119,12 @@ inline int prepare_attend(const rrq_cache *cache, const rrq_batch *batch, const 
     a.causal = c.causal;
     a.q_bf16 = c.q_dtype == RRQ_BF16;
     a.out_bf16 = c.out_dtype == RRQ_BF16;
-    const AttendPlan p = attend_plan(*cache, *batch, c.n_heads, c.window);
+    AttendPlan p = attend_plan(*cache, *batch, c.n_heads, c.window, tree);
+    if (tree) {
+        // the workspace is that of the other calls on this batch
+        const int most = attend_plan(*cache, *batch, c.n_heads, 0).splits;
+        if (p.splits > most) p.splits = most;
+    }
     a.n_splits = p.splits;
     a.target = p.target;
     a.min_tiles = p.min_tiles;

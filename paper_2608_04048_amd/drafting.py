@@ -147,7 +147,7 @@ def _matrix(t, name: str, rows: int, cols: int, index: int) -> int:
         raise TypeError(f"{name} must be a torch.Tensor")
     if t.get_device() != index:
         raise ValueError(f"{name} must be on cuda:{index}, got {t.device}")
-    if tuple(t.shape) != (rows, cols):
+    if t.shape != (rows, cols):
         raise ValueError(f"{name} must be {(rows, cols)}, got {tuple(t.shape)}")
     stride, one = t.stride()
     if one != 1 and cols > 1:
@@ -160,7 +160,7 @@ def _vector(t, name: str, cols: int, dtype, index: int):
     if t is None:
         return None
     if (not isinstance(t, torch.Tensor) or t.dtype != dtype or t.get_device() != index or
-            tuple(t.shape) != (cols,) or not t.is_contiguous()):
+            t.shape != (cols,) or not t.is_contiguous()):
         raise ValueError(f"{name} must be a contiguous {dtype} tensor [{cols}] on cuda:{index}")
     return t.data_ptr()
 
@@ -224,9 +224,12 @@ def block_norm(residual, y=None, weight=None, bias=None, kind: str = "rms", post
     if out is None:
         out_dtype = torch.bfloat16 if out_dtype is None else out_dtype
         out_code = _dtype_code(out_dtype, "out_dtype")
-        x = torch.empty((rows, cols), dtype=out_dtype, device=residual.device)
-        h = residual if y is None else torch.empty((rows, cols), dtype=residual.dtype,
-                                                   device=residual.device)
+        if not residual.is_contiguous():
+            h = torch.empty((rows, cols), dtype=residual.dtype, device=residual.device)
+        else:
+            h = torch.empty_like(residual)      # (quicker)
+        x = torch.empty_like(h, dtype=out_dtype)
+        h = h if y is not None else residual
     else:
         x, h = out
         for t, name in ((x, "out[0]"), (h, "out[1]")):
@@ -457,7 +460,7 @@ def verify_drafts(logits, tokens, offsets, max_accept: int, uniforms, draft=None
         if draft.numel() > 0:
             draft_ptr = draft.data_ptr()
     counts = torch.empty(n_seqs, dtype=torch.int32, device=logits.device)
-    following = torch.empty(n_seqs, dtype=torch.int64, device=logits.device)
+    following = torch.empty_like(counts, dtype=torch.int64)     # (quicker)
     paths = torch.empty((n_seqs, max_accept + 1), dtype=torch.int32, device=logits.device)
     if workspace is None:
         workspace = _workspace(_verify_bytes(logits, n_seqs, draft), logits.device)
