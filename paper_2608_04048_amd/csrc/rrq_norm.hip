@@ -4,6 +4,11 @@
 //
 // One workgroup takes a row and holds it in registers, so that the mean and then
 // the squares of the differences to it are summed from the exact elements.
+//
+// Memory bounds many rows: 16384 of 4096 (bfloat16 residual and result, binary32
+// output of the block) 117 us, 5.7 TB/s; with a gate of rows and a post norm, 16384 of
+// 5120, 234 us, 5.0. Few rows are latency: one of 4096 2.8 us, 300 of 5120 with gate,
+// post norm and layer norm (three sums) 8.1 us where their bytes need 4.6.
 #include <hip/hip_runtime.h>
 
 #include "rrq_draft_launch.h"
@@ -225,8 +230,10 @@ hipError_t norm_pieces(const BlockNorm &a, bool r_bf16, bool y_bf16, unsigned th
 
 hipError_t launch_block_norm(const BlockNorm &a, bool r_bf16, bool y_bf16, hipStream_t stream)
 {
+    // One piece a thread as far as 1024 threads reach: 300 rows of 5120, gated with a
+    // post norm, 8.1 us (8.5 with two), 16384 of them 234 (302).
     const int pieces = (a.hidden + kPiece - 1) / kPiece;
-    const int ch = pieces <= 512 ? 1 : (pieces <= 2048 ? 2 : (pieces <= 4096 ? 4 : 8));
+    const int ch = pieces <= 1024 ? 1 : (pieces <= 2048 ? 2 : (pieces <= 4096 ? 4 : 8));
     const unsigned threads = ((pieces + ch - 1) / ch + 63) / 64 * 64;
     switch (ch) {
     case 1: return norm_pieces<1>(a, r_bf16, y_bf16, threads, stream);
