@@ -413,10 +413,11 @@ __device__ __forceinline__ double lane_value(double x, int i)
     return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
 
-// Step 2: one workgroup a sequence. Of 64 rows at a time, kRowLanes lanes a row find
-// the token's probability under its parent; the first wave walks.
-constexpr int kDecideThreads = 64 * kRowLanes;
-__global__ __launch_bounds__(kDecideThreads) void verify_decide_kernel(Verify a)
+// Step 2, by a workgroup of T threads: where the walk of sequence b ends. Of 64 rows at
+// a time, kRowLanes lanes a row find the token's probability under its parent; the first
+// wave walks. write: whether this workgroup writes what is known then.
+template <int T>
+__device__ __forceinline__ VerifyChoice decide(const Verify &a, int b, bool write)
 {
     struct Row {
         double w, q, l, lq;
@@ -424,19 +425,19 @@ __global__ __launch_bounds__(kDecideThreads) void verify_decide_kernel(Verify a)
     };
     __shared__ Row rows[64];
     __shared__ int at_shared, count_shared, rejected_shared;
-    const int b = blockIdx.x, t = threadIdx.x, lane = t & 63;
+    const int t = threadIdx.x, lane = t & 63;
     const bool greedy = a.inv_temperature == 0.0, given = a.draft && !greedy;
     int n;
     const int o0 = rows_of(a, b, n);
     int32_t *path = a.paths + (int64_t)b * (a.max_accept + 1);
-    for (int i = t; i <= a.max_accept; i += kDecideThreads) path[i] = i == 0 && n > 0 ? 0 : -1;
+    for (int i = t; write && i <= a.max_accept; i += T) path[i] = i == 0 && n > 0 ? 0 : -1;
     const double c = kLog2e * a.inv_temperature, cq = kLog2e * a.inv_draft_temperature;
     int at = 0, count = 0, rejected = -1;
     double mass = 1.0;
     for (int base = 0; base < n && count < a.max_accept && rejected < 0; base += 64) {
-        const int k = t / kRowLanes;
-        if (const int parent = base + k < n ? parent_of(a, o0, base + k) : -1; parent >= 0) {
-            const int j = base + k;
+        for (int k = t / kRowLanes; k < 64 && base + k < n; k += T / kRowLanes) {
+            const int j = base + k, parent = parent_of(a, o0, j);
+            if (parent < 0) continue;
             const int64_t token = a.tokens[o0 + j];
             const bool inside = token >= 0 && token < a.vocab;
             Row r = {};
@@ -484,7 +485,7 @@ __global__ __launch_bounds__(kDecideThreads) void verify_decide_kernel(Verify a)
                     at = base + i;
                     mass = 1.0;
                     ++count;
-                    if (lane == 0) path[count] = at;
+                    if (write && lane == 0) path[count] = at;
                     if (count == a.max_accept) break;
                     tried = __ballot(parent == at);
                     continue;
@@ -528,12 +529,21 @@ __global__ __launch_bounds__(kDecideThreads) void verify_decide_kernel(Verify a)
         following = row_best(a, choice.row);
         if (following >= a.vocab) following = -1;
     }
-    if (t == 0) {
+    if (write && t == 0) {
         a.counts[b] = count;
         if (greedy || n == 0) a.following[b] = following;
         a.choices[b] = choice;
     }
+    return choice;
 }
+
+// One workgroup a sequence.
+constexpr int kDecideThreads = 64 * kRowLanes;
+__global__ __launch_bounds__(kDecideThreads) void verify_decide_kernel(Verify a)
+{
+    decide<kDecideThreads>(a, blockIdx.x, true);
+}
+
 
 // A thread's logits v of block `seg` of the sequence's row, and with a rejected draft
 // the draft's, y. RUNS: as in place(). A token that was taken out is -inf.
@@ -574,8 +584,12 @@ __device__ __forceinline__ double weight_factor(double inv_temperature)
     return kTable * kLog2e * inv_temperature;
 }
 
-// Step 3: one workgroup a block of the vocabulary.
-template <bool BF16>
+// Step 3: one workgroup a block of the vocabulary. DECIDE: each of a sequence's decides
+// for itself first, which in few sequences takes no longer than a kernel before this
+// one and saves its launch. (Letting the workgroup that ends last go on with step 4
+// would save another, but its fences write the L2 caches back: 20 us for 20 with one
+// sequence, 225 for 102 with 96.)
+template <bool BF16, bool DECIDE>
 __global__ __launch_bounds__(kThreads) void verify_weights_kernel(Verify a)
 {
     constexpr int W = kThreads / 64;
@@ -583,7 +597,7 @@ __global__ __launch_bounds__(kThreads) void verify_weights_kernel(Verify a)
     __shared__ double lds[4][W], table[kTable];
     const int b = blockIdx.x / (uint32_t)a.draw_segments;
     const int seg = blockIdx.x % (uint32_t)a.draw_segments;
-    const VerifyChoice c = a.choices[b];
+    const VerifyChoice c = DECIDE ? decide<kThreads>(a, b, seg == 0) : a.choices[b];
     if (c.row < 0) return;
     float v[kWeightLane], y[kWeightLane];
     load_logits<BF16, false, kThreads>(a, b, c, seg, v, y);
@@ -808,10 +822,14 @@ hipError_t launch_type(const Verify &a, hipStream_t stream)
         else
             verify_sums_kernel<BF16, false><<<grid, kThreads, 0, stream>>>(a);
     }
-    verify_decide_kernel<<<(unsigned)a.n_seqs, kDecideThreads, 0, stream>>>(a);
+    const unsigned blocks = (unsigned)(a.n_seqs * a.draw_segments);
+    const bool few = !greedy && blocks <= kServeCus;
+    if (!few) verify_decide_kernel<<<(unsigned)a.n_seqs, kDecideThreads, 0, stream>>>(a);
     if (!greedy) {
-        verify_weights_kernel<BF16>
-            <<<(unsigned)(a.n_seqs * a.draw_segments), kThreads, 0, stream>>>(a);
+        if (few)
+            verify_weights_kernel<BF16, true><<<blocks, kThreads, 0, stream>>>(a);
+        else
+            verify_weights_kernel<BF16, false><<<blocks, kThreads, 0, stream>>>(a);
         verify_draw_kernel<BF16><<<(unsigned)a.n_seqs, kDrawThreads, 0, stream>>>(a);
     }
     return hipGetLastError();
