@@ -558,7 +558,15 @@ AttendPlan attend_plan(const rrq_cache &c, const rrq_batch &b, int n_heads, int6
     // workgroups resident a compute unit, ranges of 512 keys: 4800 rows on 3000
     // positions 35, and 43 of 256 keys.
     const bool full = units > kServeCus + kServeCus / 4;
-    if (p.rows_form) {
+    // Trees without a window (packed, rrq_attention_rows.hip): about what is resident at
+    // once, of 512 keys. Heads of 128, 16 trees of 40 to 65 rows on 300 to 9000, and one
+    // of 130 on 20000: 180 and 83 us at 480, 181 and 86 at 448, 180 and 91 at 512; 4 of 20
+    // to 33 on 500 to 4000: 29.7 in ranges of 512 keys, 36.5 of 320. Heads of 64, the first:
+    // 119 at 768, 127 at 512; of 256, 16 trees of 9 to 17: 70 at 480, 91 at 768.
+    if (p.rows_form && tree && window == 0) {
+        p.target = c.head_dim == 64 ? 768 : 480;
+        p.min_tiles = 8;
+    } else if (p.rows_form) {
         p.target = c.head_dim == 64 ? 640 : (full ? 768 : 384);
         p.min_tiles = c.head_dim == 64 ? 8 : (full ? 16 : 4);
     } else {

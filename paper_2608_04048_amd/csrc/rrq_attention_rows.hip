@@ -76,53 +76,51 @@ __device__ __forceinline__ int channel_of(int slot)
 // KEYS: keys of a tile, 32 or 64; PARTS: of an operand (rrq_attention.h), two of
 // which take the registers of a whole wave a SIMD; TREE: rows see of their step what
 // their bits say.
-template <int D, int CODE, int KEYS, int PARTS, bool TREE>
-__global__ __launch_bounds__(256, PARTS > 1 ? 1 : 2) void attend_rows_kernel(Attend a)
-{
+template <int D, int KEYS>
+struct RowsLds {
     // LDS bytes of a row. 16 more than a multiple of 128, so that 8 rows span all
     // banks (values of 32-key tiles: 80, an odd number of 16s, which does as well).
-    constexpr int KROW = D * 2 + 16, VROW = KEYS * 2 + 16;
-    constexpr int KB = KEYS * KROW, VB = D * VROW;
-    constexpr int BUF = KB + VB + 64;       // and the scales of its runs
-    constexpr int R = kRowsTile;
+    static constexpr int KROW = D * 2 + 16, VROW = KEYS * 2 + 16;
+    static constexpr int KB = KEYS * KROW, VB = D * VROW;
+    static constexpr int BUF = KB + VB + 64;        // and the scales of its runs
+};
+
+// Keys that any row and that every row of a row tile sees, and a range of 64-key tiles.
+struct KeyRange {
+    int lo_any, hi_any, lo_all, hi_all;
+    int tb, te;
+};
+
+// A row tile of a kv head over the key tiles [tb, te): its result (alone) or its share
+// of it, number `split` of the ranges.
+template <int D, int CODE, int KEYS, int PARTS, bool TREE>
+__device__ __forceinline__ void attend_rows(const Attend &a, const RowTile &r, int kvh,
+                                            const KeyRange &range, int split, bool alone,
+                                            uint8_t *lds)
+{
+    using Lds = RowsLds<D, KEYS>;
+    constexpr int KROW = Lds::KROW, VROW = Lds::VROW, KB = Lds::KB, VB = Lds::VB, BUF = Lds::BUF;
     constexpr float kSlack = slack(PARTS);
     constexpr int KT = KEYS * D / 16 / 256;    // 16-code pieces a thread stages
     constexpr int ND = D / 32, NK = D / 16, NH = KEYS / 32, RUNS = KEYS / 16;
-    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * BUF];
 
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 31, hb = lane >> 5;
     const int H = a.cache.n_kv_heads, P = a.cache.page_size;
-    // heads are the fastest index: workgroups go to the 8 XCDs in turn, so a
-    // head's workgroups share an L2 (at 8 heads); the last rows, which see the
-    // most keys, come first
-    const int kvh = blockIdx.x % H;
-    RowTile r;
-    if (!find_rows<R>(a, gridDim.x / H - 1 - blockIdx.x / H, r)) return;
-
     const int row = r.row0 + 32 * wave + col;
     const bool live = row < r.n_rows;
     const RowPlace place = place_of(a, live ? row : r.n_rows - 1);
     const int64_t token = place.token;
     const int head = kvh * a.ratio + place.member;
-    int lo, hi, lo_any, hi_any, lo_all, hi_all;
-    if (TREE) {
+    int lo, hi;
+    if (TREE)
         row_past(a, r, place.token, lo, hi);
-        tile_past<R>(a, r, lo_any, hi_any, lo_all, hi_all);
-    } else {
+    else
         row_keys(a, r, place.token, lo, hi);
-        tile_keys<R>(a, r, lo_any, hi_any, lo_all, hi_all);
-    }
-    int tb, te;
-    const bool alone = split_tiles<R>(a, lo_any, hi_any, blockIdx.y, tb, te);
-    if (alone && blockIdx.y > 0) return;
-    if (!alone && te <= tb) {
-        empty_range<R>(a, r, kvh, blockIdx.y);
-        return;
-    }
-    tb *= kTileKeys / KEYS;                 // to tiles of KEYS
-    te *= kTileKeys / KEYS;
+    const int lo_any = range.lo_any, hi_any = range.hi_any;
+    const int lo_all = range.lo_all, hi_all = range.hi_all;
+    const int tb = range.tb * (kTileKeys / KEYS), te = range.te * (kTileKeys / KEYS);
     const int32_t *table = a.batch.page_table + r.seq * a.batch.table_stride;
 
     // queries: lane (col, hb) holds 8 channels of its row a product, in the
@@ -396,7 +394,7 @@ __global__ __launch_bounds__(256, PARTS > 1 ? 1 : 2) void attend_rows_kernel(Att
     const float norm = mean_factor(vref, l);
     if (alone && a.n_splits > 1 && hb == 0) a.part_ml[2 * at + 1] = kAlone;
     if (!alone) {
-        const int64_t part = (int64_t)blockIdx.y * a.batch.n_tokens * a.n_heads + at;
+        const int64_t part = (int64_t)split * a.batch.n_tokens * a.n_heads + at;
         if (hb == 0) {
             a.part_ml[2 * part] = m;
             a.part_ml[2 * part + 1] = l;
@@ -426,12 +424,125 @@ __global__ __launch_bounds__(256, PARTS > 1 ? 1 : 2) void attend_rows_kernel(Att
         }
 }
 
+template <int D, int CODE, int KEYS, int PARTS, bool TREE>
+__global__ __launch_bounds__(256, PARTS > 1 ? 1 : 2) void attend_rows_kernel(Attend a)
+{
+    constexpr int R = kRowsTile;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * RowsLds<D, KEYS>::BUF];
+    const int H = a.cache.n_kv_heads;
+    // heads are the fastest index: workgroups go to the 8 XCDs in turn, so a
+    // head's workgroups share an L2 (at 8 heads); the last rows, which see the
+    // most keys, come first
+    const int kvh = blockIdx.x % H;
+    RowTile r;
+    if (!find_rows<R>(a, gridDim.x / H - 1 - blockIdx.x / H, r)) return;
+    KeyRange k;
+    if (TREE)
+        tile_past<R>(a, r, k.lo_any, k.hi_any, k.lo_all, k.hi_all);
+    else
+        tile_keys<R>(a, r, k.lo_any, k.hi_any, k.lo_all, k.hi_all);
+    const bool alone = split_tiles<R>(a, k.lo_any, k.hi_any, blockIdx.y, k.tb, k.te);
+    if (alone && blockIdx.y > 0) return;
+    if (!alone && k.te <= k.tb) {
+        empty_range<R>(a, r, kvh, blockIdx.y);
+        return;
+    }
+    attend_rows<D, CODE, KEYS, PARTS, TREE>(a, r, kvh, k, blockIdx.y, alone, lds);
+}
+
+// Trees without a window. The ranges of a sequence's row tiles are all cut alike then, so
+// a workgroup finds its own by counting through the sequences, and those that have one
+// come first. In the other kernel's grid of row tiles and ranges they stand between
+// workgroups that end at once, which leaves them unevenly spread over the compute units:
+// 16 trees of 40 to 65 rows on 300 to 9000 positions, 40 heads on 8 of 128, 200 us there
+// and 180 here; 32 of 9 to 17 rows 158 and 133; one of 130 rows on 20000, 32 heads, 96 and
+// 83. (Built and dropped: one even share of all key tiles a workgroup, that ends one row
+// tile's range and begins another's. Starting a range costs some 10 us: 212 us.)
+template <int D, int CODE, int KEYS, int PARTS>
+__global__ __launch_bounds__(256, PARTS > 1 ? 1 : 2) void attend_packed_kernel(Attend a)
+{
+    constexpr int R = kRowsTile;
+    __shared__ __attribute__((aligned(16))) uint8_t lds[2 * RowsLds<D, KEYS>::BUF];
+    const int H = a.cache.n_kv_heads, lane = threadIdx.x & 63, seqs = (int)a.batch.n_seqs;
+    const float share = fmaxf(batch_tiles<R>(a) * (float)H / (float)a.target, (float)a.min_tiles);
+    auto rows_of = [&](int s) {
+        const int n = clamp_row(a.batch, s + 1) - clamp_row(a.batch, s);
+        return n > 0 ? n * a.ratio : 0;
+    };
+    auto tiles_of = [&](int s) {
+        return (clamp_length(a, a.batch.lengths[s]) + kTileKeys - 1) / kTileKeys;
+    };
+    // ranges of a row tile of so many key tiles (as split_tiles cuts them)
+    auto ranges_of = [&](int tiles) {
+        if ((float)tiles <= 1.5f * share) return 1;
+        const float want = floorf((float)tiles / share + 0.5f);
+        return want < (float)a.n_splits ? (int)want : a.n_splits;
+    };
+    int s = -1;
+    uint32_t at = blockIdx.x;
+    for (int s0 = 0; s0 < seqs; s0 += 64) {
+        const int i = s0 + lane;
+        const uint32_t own = i < seqs ? (uint32_t)H * ((rows_of(i) + R - 1) / R) *
+                                            ranges_of(tiles_of(i)) : 0;
+        uint32_t sum = own;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const uint32_t x = __shfl_up(sum, d);
+            if (lane >= d) sum += x;
+        }
+        const uint64_t past = __ballot(sum > at);
+        if (past) {
+            const int k = __builtin_ctzll(past);
+            s = s0 + k;
+            at -= __shfl(sum - own, k);
+            break;
+        }
+        at -= __shfl(sum, 63);
+    }
+    if (s < 0) return;
+    s = uniform(s);
+    at = uniform((int)at);
+    const int tiles = uniform(tiles_of(s)), n = uniform(ranges_of(tiles));
+    const int per = (tiles + n - 1) / n;
+    RowTile r;
+    r.seq = s;
+    r.o0 = uniform(clamp_row(a.batch, s));
+    r.n_rows = uniform(rows_of(s));
+    const int given = uniform(a.batch.lengths[s]), len = given < 0 ? 0 : given;
+    r.start = len - r.n_rows / a.ratio;
+    r.len = clamp_length(a, len);
+    const int row_tiles = (r.n_rows + R - 1) / R;
+    const int kvh = at % H, split = at / H / row_tiles;
+    r.row0 = at / H % row_tiles * R;
+    KeyRange k;
+    k.lo_any = k.lo_all = 0;
+    k.hi_any = r.len;
+    k.hi_all = r.start < 0 ? 0 : (r.start < r.len ? r.start : r.len);
+    k.tb = split * per < tiles ? split * per : tiles;
+    k.te = k.tb + per < tiles ? k.tb + per : tiles;
+    const bool alone = n == 1;
+    if (split == 0 && !alone)
+        for (int i = n; i < a.n_splits; ++i) empty_range<R>(a, r, kvh, i);
+    if (!alone && k.te <= k.tb) {
+        empty_range<R>(a, r, kvh, split);
+        return;
+    }
+    attend_rows<D, CODE, KEYS, PARTS, true>(a, r, kvh, k, split, alone, lds);
+}
+
 template <int D, int CODE, bool TREE>
 hipError_t rows_code(const Attend &a, hipStream_t stream)
 {
     const dim3 grid((unsigned)(attend_row_tiles(a.batch, a.ratio, kRowsTile) *
                                a.cache.n_kv_heads), a.n_splits);
     constexpr int KEYS = D == 256 ? 32 : 64;
+    if (TREE && a.window == 0 && (int64_t)grid.x * grid.y < (int64_t(1) << 24)) {
+        if (a.out_bf16)
+            attend_packed_kernel<D, CODE, KEYS, 1><<<grid.x * grid.y, 256, 0, stream>>>(a);
+        else
+            attend_packed_kernel<D, CODE, KEYS, 2><<<grid.x * grid.y, 256, 0, stream>>>(a);
+        return hipGetLastError();
+    }
     if (a.out_bf16)
         attend_rows_kernel<D, CODE, KEYS, 1, TREE><<<grid, 256, 0, stream>>>(a);
     else
