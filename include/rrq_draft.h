@@ -115,7 +115,7 @@ typedef struct rrq_rotary {
  *   n_heads    query heads, 1..2^16 (any number).
  *   Q_out      device, dtype [n_tokens][n_heads][head_dim] contiguous, 16-byte
  *              aligned (written): the queries rotated. May be Q itself, where that is
- *              contiguous. Rows outside offsets[0]..offsets[n_seqs]-1 are not written.
+ *              contiguous, and overlaps nothing else. Rows outside offsets[0]..offsets[n_seqs]-1 are not written.
  *
  * With c = fl(amplitude cos t), s = fl(amplitude sin t) of the angle t in 64 bits,
  * fl() one binary32 rounding, a pair (x, y) becomes

@@ -14,7 +14,7 @@ struct BlockNorm {
     rrq_norm norm;
     const void *residual, *y, *gate;
     void *out, *h;
-    int64_t r_stride, y_stride, gate_stride, n_rows;
+    int64_t r_stride, y_stride, gate_stride, n_rows, row0;
     int32_t hidden, out_bf16;
 };
 hipError_t launch_block_norm(const BlockNorm &a, bool r_bf16, bool y_bf16, hipStream_t stream);

@@ -137,7 +137,7 @@ template <int CH, bool R16, bool Y16>
 __global__ __launch_bounds__(1024) void block_norm_kernel(BlockNorm a)
 {
     __shared__ float lds[64];
-    const int64_t row = blockIdx.x;
+    const int64_t row = a.row0 + blockIdx.x;
     const int N = a.hidden;
     const float inv_n = 1.0f / (float)N;
     auto first = [&](int c) { return kPiece * (int)(c * blockDim.x + threadIdx.x); };
@@ -211,19 +211,25 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(BlockNorm a)
 }
 
 template <int CH>
-hipError_t norm_pieces(const BlockNorm &a, bool r_bf16, bool y_bf16, unsigned threads,
+hipError_t norm_pieces(BlockNorm a, bool r_bf16, bool y_bf16, unsigned threads,
                        hipStream_t stream)
 {
-    const unsigned grid = (unsigned)a.n_rows;
-    if (r_bf16 && y_bf16)
-        block_norm_kernel<CH, true, true><<<grid, threads, 0, stream>>>(a);
-    else if (r_bf16)
-        block_norm_kernel<CH, true, false><<<grid, threads, 0, stream>>>(a);
-    else if (y_bf16)
-        block_norm_kernel<CH, false, true><<<grid, threads, 0, stream>>>(a);
-    else
-        block_norm_kernel<CH, false, false><<<grid, threads, 0, stream>>>(a);
-    return hipGetLastError();
+    // (a grid has 2^32 threads at most)
+    constexpr int64_t kMost = 1 << 20;
+    for (a.row0 = 0; a.row0 < a.n_rows; a.row0 += kMost) {
+        const unsigned grid = (unsigned)(a.n_rows - a.row0 < kMost ? a.n_rows - a.row0 : kMost);
+        if (r_bf16 && y_bf16)
+            block_norm_kernel<CH, true, true><<<grid, threads, 0, stream>>>(a);
+        else if (r_bf16)
+            block_norm_kernel<CH, true, false><<<grid, threads, 0, stream>>>(a);
+        else if (y_bf16)
+            block_norm_kernel<CH, false, true><<<grid, threads, 0, stream>>>(a);
+        else
+            block_norm_kernel<CH, false, false><<<grid, threads, 0, stream>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace

@@ -114,6 +114,23 @@ def test_many_rows(gpu):
     check(gpu, make(3000, 260, "bf16", "bf16", gate="rows", post="layer"), "rms")
 
 
+def test_more_rows_than_workgroups(gpu):
+    """Every row of 2^20 and some is done, the last as the first."""
+    import torch
+    rows = (1 << 20) + 70
+    a = make(70, 8, gate="rows", post="rms")
+    want, want_h = gpu.block_norm(**a)
+    far = {k: torch.zeros((rows, 8), device="cuda", dtype=a[k].dtype)
+           for k in ("residual", "y", "gate")}
+    for t, name in ((far[k], k) for k in far):
+        t[:70] = a[name]
+        t[-70:] = a[name]
+    got, h = gpu.block_norm(**{**a, **far})
+    for part in (slice(0, 70), slice(rows - 70, rows)):
+        assert torch.equal(got[part], want) and torch.equal(h[part], want_h)
+    assert (h[70:-70] == 0).all() and (got[70:-70] == 0).all()
+
+
 def test_no_rows(gpu):
     import torch
     x = torch.empty((0, 64), device="cuda")

@@ -154,6 +154,13 @@ def test_rows_that_see_nothing_are_zeros(gpu):
     got, want = run(s, 3, sets)
     assert (got[:7] == 0).all() and (got[12::2] == 0).all()
     assert (np.abs(got[7:11]).max(axis=(1, 2)) > 0).all()
+    # many rows, beside a sequence long enough to be cut
+    s = Setup(gpu, [(70, 0), (70, 3), (100, 3000), (0, 0), (66, 66)], 4, 64, 16, "int8",
+              seed=44).fill()
+    sets = trees(s)
+    sets[-66:] = [set() if i % 2 else {i} for i in range(66)]
+    got, want = run(s, 16, sets)
+    assert (got[:70] == 0).all() and (got[70:137] == 0).all() and (got[241::2] == 0).all()
 
 
 @pytest.mark.parametrize("kv", [1, 4])
