@@ -112,14 +112,17 @@ inline int prepare_attend(const rrq_cache *cache, const rrq_batch *batch, const 
     a.q_token = c.q_token_stride;
     a.q_head = c.q_head_stride;
     a.out = c.out;
-    a.window = c.window;
+    // (lengths and positions have 32 bits: a longer window hides no key, and its sums
+    // with them would pass 64)
+    const int64_t window = c.window < (int64_t(1) << 33) ? c.window : int64_t(1) << 33;
+    a.window = window;
     a.scale = c.scale;
     a.n_heads = c.n_heads;
     a.ratio = c.n_heads / cache->n_kv_heads;
     a.causal = c.causal;
     a.q_bf16 = c.q_dtype == RRQ_BF16;
     a.out_bf16 = c.out_dtype == RRQ_BF16;
-    AttendPlan p = attend_plan(*cache, *batch, c.n_heads, c.window, tree);
+    AttendPlan p = attend_plan(*cache, *batch, c.n_heads, window, tree);
     if (tree) {
         // the workspace is that of the other calls on this batch
         const int most = attend_plan(*cache, *batch, c.n_heads, 0).splits;

@@ -110,6 +110,22 @@ def test_any_positions(gpu):
     run(s, 40, trees(s), 50, [far[i % 8] for i in range(54)])
 
 
+@pytest.mark.parametrize("window", [(1 << 32) - 1, 1 << 32, 1 << 33, (1 << 63) - 1])
+@pytest.mark.parametrize("seqs", [FEW, MANY])
+def test_windows_longer_than_any_position(gpu, window, seqs):
+    """They hide no key of a row at any position, in either attention."""
+    import torch
+    s = Setup(gpu, seqs, 1, 64, 16, "int8", seed=8).fill()
+    low = -(1 << 31) if window > 1 << 32 else 0
+    run(s, 4, trees(s), window, [(low, -1, 0, (1 << 31) - 1)[i % 4] if low else i % 4
+                                 for i in range(s.offsets[-1])])
+    Q = torch.randn((s.offsets[-1], 4, 64), device="cuda")
+    got = gpu.cache_attention(s.cache, s.batch, Q, window=window, out_dtype=torch.float32)
+    want = gpu.cache_attention(s.cache, s.batch, Q, out_dtype=torch.float32)
+    # (ranges may be cut elsewhere; operands have 22 bits, scores are below 12)
+    assert (got - want).abs().max() <= 2.0 ** -17 * want.abs().max()
+
+
 @pytest.mark.parametrize("seqs", [FEW, MANY, [(100, 1000)]])
 @pytest.mark.parametrize("dim", [64, 128, 256])
 def test_a_chain_is_causal_attention(gpu, seqs, dim):
