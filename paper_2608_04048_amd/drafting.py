@@ -224,10 +224,7 @@ def block_norm(residual, y=None, weight=None, bias=None, kind: str = "rms", post
     if out is None:
         out_dtype = torch.bfloat16 if out_dtype is None else out_dtype
         out_code = _dtype_code(out_dtype, "out_dtype")
-        if not residual.is_contiguous():
-            h = torch.empty((rows, cols), dtype=residual.dtype, device=residual.device)
-        else:
-            h = torch.empty_like(residual)      # (quicker)
+        h = torch.empty_like(residual, memory_format=torch.contiguous_format)
         x = torch.empty_like(h, dtype=out_dtype)
         h = h if y is not None else residual
     else:
@@ -329,7 +326,8 @@ def cache_append(cache: KVCache, batch: CacheBatch, rotary: Rotary, Q, K, V, pos
     code = _dtype_code(dtype, "Q")
     at = _check_positions(positions, rows, index)
     if out is None:
-        out = torch.empty(Q.shape, dtype=dtype, device=cache.device)
+        # (1.2 us; torch.empty with this shape and device 2.1)
+        out = torch.empty_like(Q, memory_format=torch.contiguous_format)
     else:
         _check_out(out, "out", Q.shape, dtype, index)
     st = (_lib or _library()).rrq_cache_append(
@@ -366,7 +364,7 @@ def tree_attention(cache: KVCache, batch: CacheBatch, Q, seen, positions=None, s
     if out is None:
         out_dtype = torch.bfloat16 if out_dtype is None else out_dtype
         out_code = _dtype_code(out_dtype, "out_dtype")
-        out = torch.empty(shape, dtype=out_dtype, device=cache.device)
+        out = torch.empty_like(Q, dtype=out_dtype, memory_format=torch.contiguous_format)
     else:
         out_dtype = out.dtype if out_dtype is None else out_dtype
         out_code = _dtype_code(out_dtype, "out")
