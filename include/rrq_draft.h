@@ -192,6 +192,8 @@ int rrq_tree_attention(const rrq_cache *cache, const rrq_batch *batch, const voi
  *              (another row is no one's child); NULL: a chain, j - 1.
  *   draft      device, dtype [n_seqs][max_accept][vocab] with strides in elements, or
  *              NULL. Not together with parents. Rows of absent drafts are not read.
+ *              A row of -inf, or one that holds a NaN or +inf, rejects its token, and
+ *              the next one is drawn from p.
  *   temperature, draft_temperature  2^-64 .. 2^64; temperature may be 0.
  *   max_accept 0..2^20.
  *   counts     device, int32 [n_seqs] (written): accepted drafts.

@@ -47,7 +47,7 @@ struct VerifySum {
     double sum;
 };
 struct VerifyChoice {
-    int32_t row, first, n, at;      // of the logits; of the sequence; -1: no rows
+    int32_t row, first, n, at;      // of the logits (-1: nothing to draw from); of the sequence
     int32_t draft;                  // the draft's row that was rejected, -1: none
     int32_t removed;                // the children's tokens are
     float m, mq;                    // with a rejected draft: largest logits and sums

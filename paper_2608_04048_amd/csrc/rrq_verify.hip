@@ -433,6 +433,7 @@ __device__ __forceinline__ VerifyChoice decide(const Verify &a, int b, bool writ
     };
     __shared__ Row rows[64];
     __shared__ int at_shared, count_shared, rejected_shared;
+    __shared__ bool spoilt_shared;
     const int t = threadIdx.x, lane = t & 63;
     const bool greedy = a.inv_temperature == 0.0, given = a.draft && !greedy;
     int n;
@@ -441,6 +442,9 @@ __device__ __forceinline__ VerifyChoice decide(const Verify &a, int b, bool writ
     for (int i = t; write && i <= a.max_accept; i += T) path[i] = i == 0 && n > 0 ? 0 : -1;
     const double c = kLog2e * a.inv_temperature, cq = kLog2e * a.inv_draft_temperature;
     int at = 0, count = 0, rejected = -1;
+    // A row without a distribution accepts nothing, and the weights must not be asked
+    // whether it has one: the token that spoils it may be a child's, which they leave out.
+    bool spoilt = false;
     double mass = 1.0;
     for (int base = 0; base < n && count < a.max_accept && rejected < 0; base += 64) {
         for (int k = t / kRowLanes; k < 64 && base + k < n; k += T / kRowLanes) {
@@ -485,9 +489,12 @@ __device__ __forceinline__ VerifyChoice decide(const Verify &a, int b, bool writ
                 for (uint64_t left = __ballot(sibling); left; left &= left - 1)
                     if (token == __shfl(gone, __builtin_ctzll(left)) && parent == at) w = 0.0;
             }
+            const double l = parent >= 0 ? rows[lane].l : 1.0;
+            const uint64_t none = __ballot(!(l > 0.0 && l < (double)kInf));
             uint64_t tried = __ballot(parent == at);
             while (tried) {
                 const int i = __builtin_ctzll(tried);
+                spoilt = !greedy && (none >> i & 1);
                 const double wi = lane_value(w, i), ui = lane_value(u, i);
                 if (given ? ui * lane_value(q, i) < wi : ui * mass < wi) {
                     at = base + i;
@@ -510,15 +517,17 @@ __device__ __forceinline__ VerifyChoice decide(const Verify &a, int b, bool writ
                 at_shared = at;
                 count_shared = count;
                 rejected_shared = rejected;
+                spoilt_shared = spoilt;
             }
         }
         __syncthreads();
+        spoilt = spoilt_shared;
         at = at_shared;
         count = count_shared;
         rejected = rejected_shared;
     }
     VerifyChoice choice = {};
-    choice.row = n > 0 ? o0 + at : -1;
+    choice.row = n > 0 && !spoilt ? o0 + at : -1;
     choice.first = o0;
     choice.n = n;
     choice.at = at;
@@ -539,7 +548,7 @@ __device__ __forceinline__ VerifyChoice decide(const Verify &a, int b, bool writ
     }
     if (write && t == 0) {
         a.counts[b] = count;
-        if (greedy || n == 0) a.following[b] = following;
+        if (greedy || choice.row < 0) a.following[b] = following;
         a.choices[b] = choice;
     }
     return choice;
