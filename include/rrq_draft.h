@@ -210,8 +210,9 @@ int rrq_tree_attention(const rrq_cache *cache, const rrq_batch *batch, const voi
  *              after the call; calls that may run at the same time need their own.
  * int64 arrays 8-byte aligned, int32 and float arrays 4-byte.
  *
- * Arithmetic: the next token is drawn in 64 bits; a row's sum behind an acceptance is
- * good to about 2^-24. Results are deterministic.
+ * Arithmetic: the next token is drawn in 64 bits; a row's sum behind an acceptance has
+ * binary32 exponentials and is good to 2^-24 as a rule, to 18 x 2^-24 at worst. Results
+ * are deterministic.
  *
  * Returns RRQ_OK, or RRQ_ERR_NULL / _ALIGN / _SHAPE / _DTYPE / _WORKSPACE with nothing
  * enqueued, or RRQ_ERR_HIP.

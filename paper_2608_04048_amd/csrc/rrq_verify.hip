@@ -18,7 +18,12 @@
 // that any input may come near, and the results are whole numbers. Step 1 has
 // binary32 exponentials (each off by 2^-24 or so at random) and corrects what is
 // systematic, the rounding of log2(e) / T, by the sum of e d; sums of more than eight
-// are 64 bits: l is good to about 2^-24, and a decision off in one of some 10^7 cases.
+// are 64 bits. A logit's distance d to its thread's reference is rounded, and so is its
+// product with log2(e) / T: 2^-24 of the exponent each, so the reference is the largest of
+// 2048 logits and moves up where a later one passes it by 6 powers of two. l is good to
+// 2^-24 as a rule, a decision off in one of some 10^7 cases; at worst, with all of l in one
+// such logit, to 18 x 2^-24 (2 x 6 ln 2 of those roundings, 2 of the exponential, 7 of the
+// additions). A reference that stays put until 2^60 gives 50 x 2^-24 there and saves no time.
 // Running sums of a vocabulary pass borders that lie 10^-5 apart: steps 3 and 4 are 64
 // bits throughout, exponentials good to 2 10^-13. The residual (p - q)+ needs both rows'
 // sums before it can be formed; step 3 leaves the sums of p and of q over the tokens
@@ -44,6 +49,9 @@ namespace {
 constexpr float kInf = __builtin_inff();
 constexpr double kLn2 = 0.69314718055994530942, kLog2e = 1.44269504088896340736;
 constexpr int kThreads = 256;
+// A block's sum from which on step 1's reference moves up to the block's largest logit.
+// (32 logits up to the reference make 32 at most.)
+constexpr double kFar = 64.0;
 // Logits a thread takes: in step 1; in step 3, and in step 4, whose one workgroup a
 // sequence has twice the threads, as its time is a single wave's.
 constexpr int kSumLane = 32, kWeightLane = 16, kDrawLane = 8, kDrawThreads = 512;
@@ -320,12 +328,14 @@ __global__ __launch_bounds__(kThreads) void verify_sums_kernel(Verify a)
                     s += (double)part;
                 }
             };
-            // A thread's m is the largest logit of its first block that has any: later
-            // ones need no maximum of their own until a sum says that they do.
-            if (m == -kInf) m = largest();
+            // m is the largest logit of the wave's first block that has any: later ones
+            // need no maximum of their own until a thread's sum says that they do (from
+            // its own first block, sums say so often: 113 us where this takes 96). It is
+            // -inf in all lanes or in none.
+            if (m == -kInf) m = wave_max(largest());
             if (m > -kInf) {
                 add([](float d) { return d; });
-                const bool far = !(s < 0x1p60);
+                const bool far = !(s < kFar);
                 // (a logit of -inf makes t no number; so may one that is none)
                 if (far || t != t) {
                     if (far) {
