@@ -198,7 +198,9 @@ int rrq_tree_attention(const rrq_cache *cache, const rrq_batch *batch, const voi
  *   max_accept 0..2^20.
  *   counts     device, int32 [n_seqs] (written): accepted drafts.
  *   following  device, int64 [n_seqs] (written): the next token; -1 for a sequence
- *              without rows, and where nothing is left to draw from. A row of -inf,
+ *              without rows, or that ends at a row without a distribution. Where a row's
+ *              drafts are all that it leaves possible, and the sum's last digits reject
+ *              them all, the last of them that has any probability. A row of -inf,
  *              or one that holds a NaN or +inf, accepts nothing and gives -1 (at a
  *              temperature of 0 a NaN counts as less than every number).
  *   paths      device, int32 [n_seqs][max_accept + 1] (written): row 0, then the

@@ -50,6 +50,7 @@ struct VerifyChoice {
     int32_t row, first, n, at;      // of the logits (-1: nothing to draw from); of the sequence
     int32_t draft;                  // the draft's row that was rejected, -1: none
     int32_t removed;                // the children's tokens are
+    int32_t last;                   // the last of them that had any weight, -1: none
     float m, mq;                    // with a rejected draft: largest logits and sums
     double l, lq;
 };

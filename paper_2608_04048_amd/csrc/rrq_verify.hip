@@ -442,7 +442,7 @@ __device__ __forceinline__ VerifyChoice decide(const Verify &a, int b, bool writ
         float m, mq;
     };
     __shared__ Row rows[64];
-    __shared__ int at_shared, count_shared, rejected_shared;
+    __shared__ int at_shared, count_shared, rejected_shared, last_shared;
     __shared__ bool spoilt_shared;
     const int t = threadIdx.x, lane = t & 63;
     const bool greedy = a.inv_temperature == 0.0, given = a.draft && !greedy;
@@ -451,7 +451,7 @@ __device__ __forceinline__ VerifyChoice decide(const Verify &a, int b, bool writ
     int32_t *path = a.paths + (int64_t)b * (a.max_accept + 1);
     for (int i = t; write && i <= a.max_accept; i += T) path[i] = i == 0 && n > 0 ? 0 : -1;
     const double c = kLog2e * a.inv_temperature, cq = kLog2e * a.inv_draft_temperature;
-    int at = 0, count = 0, rejected = -1;
+    int at = 0, count = 0, rejected = -1, last = -1;
     // A row without a distribution accepts nothing, and the weights must not be asked
     // whether it has one: the token that spoils it may be a child's, which they leave out.
     bool spoilt = false;
@@ -509,6 +509,7 @@ __device__ __forceinline__ VerifyChoice decide(const Verify &a, int b, bool writ
                 if (given ? ui * lane_value(q, i) < wi : ui * mass < wi) {
                     at = base + i;
                     mass = 1.0;
+                    last = -1;
                     ++count;
                     if (write && lane == 0) path[count] = at;
                     if (count == a.max_accept) break;
@@ -520,6 +521,7 @@ __device__ __forceinline__ VerifyChoice decide(const Verify &a, int b, bool writ
                     break;
                 }
                 mass -= wi;
+                if (wi > 0.0) last = base + i;
                 tried &= tried - 1;
                 if (parent == at && token == __shfl(token, i)) w = 0.0;
             }
@@ -527,10 +529,12 @@ __device__ __forceinline__ VerifyChoice decide(const Verify &a, int b, bool writ
                 at_shared = at;
                 count_shared = count;
                 rejected_shared = rejected;
+                last_shared = last;
                 spoilt_shared = spoilt;
             }
         }
         __syncthreads();
+        last = last_shared;
         spoilt = spoilt_shared;
         at = at_shared;
         count = count_shared;
@@ -544,6 +548,7 @@ __device__ __forceinline__ VerifyChoice decide(const Verify &a, int b, bool writ
     choice.draft = rejected >= 0 ? rejected - 1 : -1;
     // children were all tried and rejected
     choice.removed = !given && count < a.max_accept;
+    choice.last = last;
     if (rejected >= 0) {
         const Row &r = rows[rejected & 63];
         choice.m = r.m;
@@ -769,7 +774,11 @@ __global__ __launch_bounds__(kDrawThreads) void verify_draw_kernel(Verify a)
     }
     const double total = residual ? res : lp;
     if (!(total > 0.0) || total > 1e300) {
-        if (t == 0) a.following[b] = -1;
+        // Nothing left of a sound row: its children are all that it has. By the formulas
+        // the last one that has any probability is accepted then, and only the roundings
+        // of step 1's sum can have rejected it: it comes as the next token.
+        const bool all = total == 0.0 && c.removed && c.last >= 0;
+        if (t == 0) a.following[b] = all ? a.tokens[c.first + c.last] : -1;
         return;
     }
     const double goal = u * total;
