@@ -201,8 +201,10 @@ int rrq_tree_attention(const rrq_cache *cache, const rrq_batch *batch, const voi
  *              without rows, or that ends at a row without a distribution. Where a row's
  *              drafts are all that it leaves possible, and the sum's last digits reject
  *              them all, the last of them that has any probability. A row of -inf,
- *              or one that holds a NaN or +inf, accepts nothing and gives -1 (at a
- *              temperature of 0 a NaN counts as less than every number).
+ *              or one that holds a NaN or +inf, accepts nothing and gives -1. At a
+ *              temperature of 0 infinities are numbers as others and a NaN is less
+ *              than any: of a row of -inf the first token is accepted or given, and
+ *              only a row of nothing but NaN gives -1.
  *   paths      device, int32 [n_seqs][max_accept + 1] (written): row 0, then the
  *              accepted rows, then -1.
  *   n_rows     0..2^23; vocab 1..2^30; row_stride >= vocab; n_seqs 0..2^20 (0: nothing

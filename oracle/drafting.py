@@ -159,8 +159,8 @@ def _softmax(x, temperature):
     x = np.asarray(x, np.float64)
     if temperature == 0:
         p = np.zeros_like(x)
-        if not np.isnan(x).all():
-            p[int(np.nanargmax(x))] = 1.0
+        if not np.isnan(x).all():       # (np.nanargmax takes a NaN for -inf)
+            p[int(np.nonzero(x == np.nanmax(x))[0][0])] = 1.0
         return p
     if np.isnan(x).any() or not np.isfinite(x.max()):
         return np.full_like(x, np.nan)

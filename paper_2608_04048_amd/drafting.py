@@ -409,9 +409,11 @@ def verify_drafts(logits, tokens, offsets, max_accept: int, uniforms, draft=None
     type) gives the distributions the drafts were drawn from, logits as well; without it
     a rejected token's probability is taken out. A temperature of 0 is greedy.
 
-    counts is int32 [n_seqs], following int64 [n_seqs] (-1: none), paths int32 [n_seqs,
-    max_accept + 1]: row 0, the accepted rows in order, then -1. At most max_accept
-    drafts of a sequence are accepted."""
+    counts is int32 [n_seqs], following int64 [n_seqs], paths int32 [n_seqs, max_accept + 1]:
+    row 0, the accepted rows in order, then -1. At most max_accept drafts of a sequence are
+    accepted. following is -1 for a sequence without rows, or that ends at a row of -inf or
+    one with a NaN or +inf; at a temperature of 0 those are numbers as others (a NaN less
+    than any), a row of -inf gives token 0, and only one of nothing but NaN -1."""
     if not isinstance(logits, torch.Tensor):
         raise TypeError("logits must be a torch.Tensor")
     index = logits.get_device()

@@ -1,5 +1,6 @@
 """Target rows without a distribution (a NaN, +inf, nothing but -inf), also where what spoils
-them is the very token of a rejected child; draft rows without one."""
+them is the very token of a rejected child; draft rows without one; what greedy calls make
+of such rows."""
 
 import numpy as np
 import pytest
@@ -81,3 +82,22 @@ def test_a_draft_row_without_a_distribution_rejects(gpu):
     a["draft"][2::4, 0, 78] = np.inf
     counts, following, _ = check(gpu, (a, dtype, pad))
     assert counts.tolist() == [0, 0, 0, 1] * 2 and (following >= 0).all()
+
+
+@pytest.mark.parametrize("vocab", [5, 9000, 70001])
+def test_greedy_infinities(gpu, vocab):
+    """At a temperature of 0 the first of the largest logits, -inf and +inf being numbers
+    as others and a NaN less than any; nothing but NaN: none."""
+    a, dtype, pad = make([2] * 5, vocab, seed=45)
+    a["tokens"][1::2] = [0, 3, 4, 2, 0]
+    a["logits"][0] = -np.inf                # 0, and the draft is it
+    a["logits"][2, [3, 4]] = np.inf         # 3
+    a["logits"][4] = np.nan
+    a["logits"][4, 4] = -np.inf             # 4
+    a["logits"][6] = np.nan                 # none
+    a["logits"][8, :3] = np.nan             # the largest of the others
+    counts, following, paths = check(gpu, (a, dtype, pad), 0.0)
+    assert counts.tolist() == [1, 1, 1, 0, 0]
+    assert following[3].item() == -1
+    assert following[4].item() == 3 + int(np.argmax(a["logits"][8, 3:]))
+    assert paths.tolist()[3] == [0, -1]
