@@ -17,6 +17,7 @@
 // Memory bounds long calls: 8192 tokens of 40 query and 8 kv heads of 128 in binary32, 419
 // MB, 83 us (5.0 TB/s). The last tokens of 24 sequences 5.6 us and 16 trees of 20 to 40
 // drafts 9.3: a launch, and offsets, page and rows one after another.
+#include "rrq_append_rows.h"
 #include "rrq_cache_device.h"
 #include "rrq_draft_launch.h"
 
@@ -179,8 +180,8 @@ __device__ __forceinline__ void rotate_queries(const CacheAppend &a, int64_t tok
 {
     const int pairs = a.rot / 2, t = threadIdx.x;
     const int64_t first = clamp_row(a.batch, 0), end = clamp_row(a.batch, (int)a.batch.n_seqs);
-    int n = a.query_tokens;
-    if (token0 + n > end) n = (int)(end - token0);
+    const GroupRows g = group_rows(token0, a.query_tokens, first, end, a.n_heads);
+    const int n = g.tokens;
     // a wave's lanes share a token at a time, so that one finds its sequence
     const int wave = t >> 6, waves = blockDim.x >> 6, lane = t & 63;
     for (int k = wave; k < n; k += waves) {
@@ -202,9 +203,8 @@ __device__ __forceinline__ void rotate_queries(const CacheAppend &a, int64_t tok
     __syncthreads();
     constexpr int TPT = D / 8;
     const Unit u = unit_of(a, t % TPT);
-    const int step = blockDim.x / TPT, rows = n * a.n_heads;
-    const int k0 = token0 < first ? (int)(first - token0) * a.n_heads : 0;
-    for (int r0 = k0 + t / TPT; r0 < rows; r0 += step * kQueryRows) {
+    const int step = blockDim.x / TPT, rows = g.end;
+    for (int r0 = g.begin + t / TPT; r0 < rows; r0 += step * kQueryRows) {
         f32x4 x[kQueryRows], y[kQueryRows];
         int k[kQueryRows];
         int64_t out[kQueryRows];
