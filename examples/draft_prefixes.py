@@ -154,7 +154,8 @@ def generate(decoder, prompts, n_new, k_draft=1, k=4, widths=(1, 1, 1, 1), tempe
     n = len(prompts)
     tree, chain = Tree(widths), max(widths) == 1
     depth, n_rows = len(widths), sum(map(len, Tree(widths).levels))
-    most = max(map(len, prompts)) + n_new + n_rows + depth + 1
+    # the slowest text gains a token a step, while another may gain all its drafts
+    most = max(map(len, prompts)) + n_new * (depth + 1) + n_rows
     draft, target = (Texts(decoder, x, n, most) for x in (k_draft, k))
     texts = [list(p) for p in prompts]
     for side in (draft, target):            # all but the last tokens
