@@ -115,7 +115,8 @@ typedef struct rrq_rotary {
  *   n_heads    query heads, 1..2^16 (any number).
  *   Q_out      device, dtype [n_tokens][n_heads][head_dim] contiguous, 16-byte
  *              aligned (written): the queries rotated. May be Q itself, where that is
- *              contiguous, and overlaps nothing else. Rows outside offsets[0]..offsets[n_seqs]-1 are not written.
+ *              contiguous, and overlaps nothing else. Rows outside
+ *              offsets[0]..offsets[n_seqs]-1 are not written.
  *
  * With c = fl(amplitude cos t), s = fl(amplitude sin t) of the angle t in 64 bits,
  * fl() one binary32 rounding, a pair (x, y) becomes
@@ -141,7 +142,9 @@ int rrq_cache_append(const rrq_cache *cache, const rrq_batch *batch, const rrq_r
  *   - the step's row j (at start + j) if bit j of row i of `seen` is set, whatever
  *     the window; a row sees itself by its own bit alone. Bits of n_b and more play
  *     no part, rows past the bits are not seen.
- * A row that sees nothing gives zeros.
+ * A row that sees nothing gives zeros. All positions below the length have to have
+ * been written, the step's rows that no bit names included: those have no weight, but
+ * their codes are multiplied by it, and what a slot held before may be no number.
  *
  *   seen       device, uint64 [n_tokens][seen_words], 8-byte aligned: bit j is bit
  *              j % 64 of word j / 64.

@@ -211,7 +211,9 @@ void attend_kernel(Attend a)
         }
         // Keys a row does not see. The codes there may be left over from
         // another use of the page (not numbers, even), so scores are replaced
-        // and value codes of keys that no row sees are cleared.
+        // and value codes of keys outside every row's range are cleared. (A
+        // tree's range ends with its step, whose rows are all written, also
+        // those that no bit names.)
         if (key0 < lo_all || key0 + kTileKeys > hi_all || !__all(there)) {
 #pragma unroll
             for (int b = 0; b < NQ; ++b) {

@@ -344,8 +344,9 @@ def tree_attention(cache: KVCache, batch: CacheBatch, Q, seen, positions=None, s
     workspace, ``attention_workspace``): a row sees the positions before its
     sequence's rows of this batch (of its window, counted from its position), and of
     those rows the ones whose bits are set in its row of ``seen`` (int64 [n_tokens,
-    words], contiguous: bit j % 64 of word j // 64 is the sequence's row j). positions
-    (int32 [n_tokens]) defaults to the rows' places in their sequences."""
+    words], contiguous: bit j % 64 of word j // 64 is the sequence's row j). All rows of
+    the batch have to be in the cache, also those that no bit names. positions (int32
+    [n_tokens]) defaults to the rows' places in their sequences."""
     index = _device_index(cache, batch)
     if elsewhere(index, stream):
         used = (*cache.tensors, *batch.tensors, Q, seen, positions, workspace, out)
