@@ -27,7 +27,7 @@
 // 44 GFLOP in 105 us (420 TFLOP/s): 340 row tiles on 256 compute units, and 32-key
 // tiles, as LDS holds two workgroups' 64-key tiles of such heads no more (one a
 // compute unit: 156 us). Registers are full there: 6 (int8) and 3 (e4m3) vector
-// registers spill, and 37 scalar ones with heads of 64.
+// registers spill, of trees 8 and 6, and up to 36 scalar ones with heads of 64.
 //
 // The running maximum m moves only when a tile's exceeds it by 8 (weights
 // then grow to 2^8 at most): most tiles skip the output's rescaling.
@@ -453,10 +453,10 @@ __global__ __launch_bounds__(256, PARTS > 1 ? 1 : 2) void attend_rows_kernel(Att
 // Trees without a window. The ranges of a sequence's row tiles are all cut alike then, so
 // a workgroup finds its own by counting through the sequences, and those that have one
 // come first. In the other kernel's grid of row tiles and ranges they stand between
-// workgroups that end at once, which leaves them unevenly spread over the compute units:
-// 16 trees of 40 to 65 rows on 300 to 9000 positions, 40 heads on 8 of 128, 200 us there
-// and 180 here; 32 of 9 to 17 rows 158 and 133; one of 130 rows on 20000, 32 heads, 96 and
-// 83. (Built and dropped: one even share of all key tiles a workgroup, that ends one row
+// workgroups that end at once, which leaves them unevenly spread over the compute units.
+// The same ranges of 16 trees of 40 to 65 rows on 300 to 9000 positions, 40 heads on 8 of
+// 128, 211 to 215 us there and 181 here, with the join; of 32 of 9 to 17 rows 177 and 134;
+// of one of 130 rows on 20000, 32 heads, 82 and 81. (Built and dropped: one even share of all key tiles a workgroup, that ends one row
 // tile's range and begins another's. Starting a range costs some 10 us: 212 us.)
 template <int D, int CODE, int KEYS, int PARTS>
 __global__ __launch_bounds__(256, PARTS > 1 ? 1 : 2) void attend_packed_kernel(Attend a)

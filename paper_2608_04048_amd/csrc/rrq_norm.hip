@@ -2,12 +2,17 @@
 // post norm, gate, residual scale and addition, and the next block's norm, with
 // one read of every operand and one write of the results.
 //
-// One workgroup takes a row and holds it in registers, so that the mean and then
-// the squares of the differences to it are summed from the exact elements.
+// One workgroup takes a row and holds it, so that the mean and then the squares of the
+// differences to it are summed from the exact elements: in registers up to 32768
+// columns; of eight pieces a thread, 185 to 527 of the compiler's registers are in
+// scratch memory.
 //
 // Memory bounds many rows: 16384 of 4096 (bfloat16 residual and result, binary32
 // output of the block) 117 us, 5.7 TB/s; with a gate of rows and a post norm, 16384 of
-// 5120, 234 us, 5.0. Few rows are latency: one of 4096 2.8 us, 300 of 5120 with gate,
+// 5120, 234 us, 5.0. Longer rows, as the first without the gate (with a post norm): 4096
+// of 12288 106 us (116), 4.7 TB/s; 2048 of 20000 98 (108), 4.2; 1024 of 32768 77 (84), 4.4;
+// past that scratch memory sets the time: 1024 of 40000 173 (198), 2.4, of 65536 257 (295),
+// 2.6. Few rows are latency: one of 4096 2.8 us, 300 of 5120 with gate,
 // post norm and layer norm (three sums) 8.1 us where their bytes need 4.6.
 #include <hip/hip_runtime.h>
 

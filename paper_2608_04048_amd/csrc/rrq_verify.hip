@@ -31,12 +31,12 @@
 // step 4 to scale and subtract.
 //
 // Measured. Step 1 is bound by memory: 96 sequences of 3 to 7 drafts with the draft's
-// distributions, 150001 tokens in bfloat16, 290 MB in 58 us (5.0 TB/s), its vector
+// distributions, 150001 tokens in bfloat16, 290 MB in 59 us (4.9 TB/s), its vector
 // instructions (ten a logit) 70% of that time; of 16 trees of 29 to 48 drafts and 131072
-// tokens in binary32 the 290 rows that have children, 150 MB in 29 us. Step 3 is bound by
+// tokens in binary32 the 264 rows that have children, 138 MB in 30 us. Step 3 is bound by
 // issue: 58 MB and 14 million pairs of exponentials in 28 us, the vector units busy 72% of
 // it. Steps 2 and 4 are chains of dependent loads: 6 to 7 and 7 to 9 us. Five drafts of
-// one sequence take 3.8, 7.7 (steps 2 and 3 together) and 7.6 us.
+// one sequence take 4.0, 8.0 (steps 2 and 3 together) and 7.8 us.
 #include <hip/hip_runtime.h>
 
 #include "rrq_draft_launch.h"
@@ -618,7 +618,11 @@ __device__ __forceinline__ double weight_factor(double inv_temperature)
 
 // Step 3: one workgroup a block of the vocabulary. DECIDE: each of a sequence's decides
 // for itself first, which in few sequences takes no longer than a kernel before this
-// one and saves its launch. (Letting the workgroup that ends last go on with step 4
+// one and saves its launch: up to a block a compute unit. The call so, and with a kernel
+// before: 4 and 8 sequences of five drafts (128 and 256 blocks) 21.8 and 27.4 us, 23.6 and
+// 29.9; of trees of 29 to 48 drafts 29.0 and 34.4, 28.1 and 34.4. Past that bound 16
+// sequences 36.5 and 39.5, 16 trees 47.7 and 47.1, 32 chains of 150001 tokens 49.1 and
+// 48.2. (Letting the workgroup that ends last go on with step 4
 // would save another, but its fences write the L2 caches back: 20 us for 20 with one
 // sequence, 225 for 102 with 96.)
 template <bool BF16, bool DECIDE>
